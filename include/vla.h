@@ -316,6 +316,132 @@ void vla_backbone_destroy(vla_backbone* backbone);
 vla_status vla_prefix_prefill(vla_backbone* backbone, const void* embeds, int32_t batch, int32_t prefix_len,
                               void* hidden_out, void* stream);
 
+/* ---- 8-bit serving operators ---------------------------------------------------
+ * Operators on their own, beside vla_ternary_gemm: linear layers with int8
+ * weights, and a K/V cache in pages, in 8 bits if wanted, for requests of
+ * different lengths.  They hold no state and allocate nothing, so calls may
+ * overlap (other streams, other threads) as long as none writes what another
+ * uses, and may be captured into a HIP graph; what lies in device memory
+ * (lengths, page tables) is read when the work runs, so a replay sees its
+ * present values.  Lengths and page ids in device memory cannot be refused by
+ * the host: the kernels bound every access by what the call says, and what is
+ * said below of ids outside the pool holds.  `elem`, the type of rows that
+ * come or go: VLA_T_F32 or VLA_T_BF16.  Pitches and strides count elements.
+ * Errors of every call: VLA_E_ARG, VLA_E_SHAPE, VLA_E_UNSUPPORTED, VLA_E_DEVICE. */
+enum { VLA_T_F32 = 0, VLA_T_BF16 = 1 };
+
+/*
+ * Per-token int8 codes (the quantiser of the W2A8 linear), in fp32 arithmetic:
+ *   r[m] = max(max_k |x[m][k]|, 1e-5),  q[m][k] = rne(x[m][k] * fl(127 / r[m]))
+ * x: [M][ldx] in elem, q: [M][ldq] int8 (columns K .. ldq-1 are left as they
+ * were), r: [M] fp32.  A row with a NaN or an infinity gets codes 0 and
+ * r = NaN, so that its products are NaN.  M, K >= 0; ldx, ldq >= K.
+ */
+vla_status vla_quantize_tokens(int32_t elem, const void* x, int32_t M, int32_t K, int64_t ldx, int8_t* q,
+                               int64_t ldq, float* r, void* stream);
+
+/*
+ * W8A8 linear: y[m][n] = (sum_k q[m][k] w[n][k]) * (w_scale[n] * r[m] / 127) + bias[n],
+ * the sum exact in int32.
+ *   q [M][ldq] int8 and r [M] fp32 as vla_quantize_tokens gives them;
+ *   w [N][ldw] int8, w_scale [N] fp32 (the value of one code of that channel);
+ *   bias [N] fp32 or NULL; y [M][ldy] in elem, columns N .. ldy-1 left as they were.
+ * K, ldq and ldw are multiples of 16, K <= 131056 (so |sum| < 2^31).  M, N >= 0;
+ * K == 0 gives the bias.
+ */
+vla_status vla_int8_gemm(const int8_t* q, int64_t ldq, const float* r, const int8_t* w, int64_t ldw,
+                         const float* w_scale, const float* bias, int32_t M, int32_t N, int32_t K, int32_t elem,
+                         void* y, int64_t ldy, void* stream);
+
+/* Element type of a page: the values themselves, or 8-bit codes with one fp32
+ * scale for each row (token and K/V head) of K and of V:
+ *   value = code * scale, scale = fl(r / top), code = rne(x * fl(top / r)),
+ *   r = max(max |x| over the row, 1e-5), top = 127 (I8) or 448 (E4M3, the
+ *   8-bit float with 4 exponent bits, no infinity).
+ * A row with a NaN or an infinity is stored as code 0 with scale NaN. */
+typedef enum { VLA_KV_F32 = 0, VLA_KV_BF16 = 1, VLA_KV_I8 = 2, VLA_KV_E4M3 = 3 } vla_kv_type;
+
+/* A pool of pages.  The caller allocates it; any page may belong to any
+ * request, and several requests may read one page. */
+typedef struct vla_kv_pages {
+  int32_t type;         /* vla_kv_type */
+  int32_t n_pages;      /* pages of the pool */
+  int32_t page_size;    /* rows (tokens) of a page: a power of two, 16 .. 1024 */
+  int32_t n_kv_heads;   /* G */
+  int32_t head_dim;     /* hd: 64, 128 or 256 (VLA_KV_F32: 64 or 128) */
+  void* k;              /* [n_pages][G][page_size][hd] */
+  void* v;
+  float* k_scale;       /* [n_pages][G][page_size]; 8-bit types only */
+  float* v_scale;
+} vla_kv_pages;
+
+/* The requests of one call.  Row j of request b lies in page
+ * page_table[b][j / page_size], row j % page_size.  New tokens are given as
+ * rows t of one array: those of request b are q_start[b] .. q_start[b+1]-1, and
+ * they are its last rows, kv_len[b] - n_b .. kv_len[b]-1, in order (n_b their
+ * number).  Rows of that array outside q_start[0] .. q_start[n_requests]-1
+ * (padding) are neither read nor written.  A negative kv_len counts as 0. */
+typedef struct vla_kv_batch {
+  int32_t n_requests;         /* 0 .. 65536 */
+  int32_t max_pages;          /* entries of a request's page table; max_pages * page_size <= 2^30 */
+  int32_t n_tokens;           /* rows of the arrays of new tokens, padding included; 0 .. 2^24 */
+  int32_t max_len;            /* the host's idea of the largest kv_len, >= 0: work is spread for it; results do
+                                 not depend on it */
+  const int32_t* page_table;  /* [n_requests][max_pages]; entries past a request's last row are not read */
+  const int32_t* kv_len;      /* [n_requests]: rows of each request, its new tokens included */
+  const int32_t* q_start;     /* [n_requests + 1], non-decreasing (not used by vla_kv_pages_read: may be NULL) */
+} vla_kv_batch;               /* these arrays: 4-byte aligned */
+
+/*
+ * Write the new tokens' keys and values into their pages, quantised as the
+ * pages are.  Token t, head g begins at k + t * token_stride + g * head_stride
+ * (in elem; both strides multiples of 16 bytes; v likewise), so the keys and
+ * values may lie inside the rows of a fused projection or be a slab of the
+ * dense cache of vla_prefix_kv_build.  Tokens whose page id is outside the
+ * pool, or whose row is negative or past the page table, are not written.  Two
+ * tokens of one call must not name the same row.
+ */
+vla_status vla_kv_pages_write(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t elem, const void* k,
+                              const void* v, int64_t token_stride, int64_t head_stride, void* stream);
+
+/*
+ * Read rows 0 .. min(kv_len[b], rows)-1 of every request back as
+ * k_out, v_out [n_requests][G][rows][hd] in elem (one layer of the dense cache
+ * that vla_denoise reads, when every request has `rows` of them); the rows
+ * behind a request's last are left as they were.  Rows of a page outside the
+ * pool, or past the page table, are NaN.
+ */
+vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t rows, int32_t elem,
+                             void* k_out, void* v_out, void* stream);
+
+/*
+ * Attention of the new tokens over the pages of their requests; write the new
+ * tokens' own keys and values first.  Token i of request b is at position
+ * p = kv_len[b] - n_b + i and sees rows j < kv_len[b] with
+ *   j <= p (causal = 1), j > p - window (window > 0; 0 = no window);
+ * query head h reads K/V head floor(h * G / n_heads), and
+ *   o = sum_j softmax_j(scale * q . k_j) v_j,   lse = ln sum_j exp(scale * q . k_j).
+ * A token that sees no row gets o = 0, lse = -infinity.  A row that a token
+ * does not see has no influence on it, whatever it holds.  A token that sees a
+ * row of a page outside the pool gets NaN, and so do all tokens of a request
+ * whose kv_len is past its page table.
+ *   q, o [n_tokens][ldq / ldo] in elem, head h at column h * hd (they may be
+ *   the same array); lse [n_tokens][n_heads] fp32 or NULL.  elem is VLA_T_F32
+ *   for VLA_KV_F32 pages and VLA_T_BF16 for the others.
+ *   n_heads a multiple of G, at most 16 G; ldq, ldo multiples of 16 bytes.
+ *   workspace: at least vla_paged_attention_workspace bytes (16-byte aligned;
+ *   may be NULL if that is 0), used until the work is done: calls that may
+ *   overlap, and captured graphs that may, need one each.
+ */
+vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, int32_t elem,
+                               const void* q, int64_t ldq, void* o, int64_t ldo, float scale, int32_t causal,
+                               int32_t window, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that vla_paged_attention needs for these sizes (the
+ * pointers in the two structs are not looked at), enough for any window.
+ * (size_t)-1 on invalid arguments. */
+size_t vla_paged_attention_workspace(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads);
+
 /* Thread-local message for the last non-OK status of this thread. */
 const char* vla_last_error(void);
 const char* vla_status_string(int32_t status);

@@ -1642,6 +1642,175 @@ vla_status vla_ternary_gemm(const int8_t* x, const uint8_t* w_packed, int32_t M,
   return VLA_OK;
 }
 
+// ---- 8-bit serving operators ------------------------------------------------
+
+namespace {
+
+// A launch has fewer than 2^32 threads.
+constexpr long long kMaxThreads = (1LL << 32) - 4096;
+
+vla_status serve_elem(int32_t elem, int* bytes) {
+  if (elem != VLA_T_F32 && elem != VLA_T_BF16) return fail(VLA_E_ARG, "elem must be VLA_T_F32 or VLA_T_BF16");
+  *bytes = elem == VLA_T_F32 ? 4 : 2;
+  return VLA_OK;
+}
+
+// The sizes of a pool and a batch, as the kernels see them.
+vla_status serve_sizes(const vla_kv_pages* p, const vla_kv_batch* b, PageArgs* a) {
+  if (!p || !b) return fail(VLA_E_ARG, "pages or batch is NULL");
+  if (p->type < VLA_KV_F32 || p->type > VLA_KV_E4M3) return fail(VLA_E_ARG, "page type %d out of range", p->type);
+  if (p->n_pages < 1 || p->n_kv_heads < 1 || b->n_requests < 0 || b->max_pages < 1 || b->n_tokens < 0 || b->max_len < 0)
+    return fail(VLA_E_SHAPE, "negative or zero size in pages or batch");
+  if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+    return fail(VLA_E_SHAPE, "page_size %d is not a power of two in 16..1024", p->page_size);
+  if (!(p->head_dim == 64 || p->head_dim == 128 || (p->head_dim == 256 && p->type != VLA_KV_F32)))
+    return fail(VLA_E_UNSUPPORTED, "head_dim %d unsupported (64, 128%s)", p->head_dim, p->type == VLA_KV_F32 ? "" : ", 256");
+  if (p->n_kv_heads > 256) return fail(VLA_E_UNSUPPORTED, "more than 256 K/V heads");
+  if (b->n_requests > 65536) return fail(VLA_E_UNSUPPORTED, "more than 65536 requests");
+  if (b->n_tokens > (1 << 24)) return fail(VLA_E_UNSUPPORTED, "more than 2^24 new tokens");
+  int lg = 4;
+  while ((1 << lg) < p->page_size) ++lg;
+  if (((long long)b->max_pages << lg) > (1LL << 30)) return fail(VLA_E_SHAPE, "max_pages * page_size > 2^30");
+  a->type = p->type; a->n_pages = p->n_pages; a->lg = lg; a->G = p->n_kv_heads; a->hd = p->head_dim;
+  a->k = p->k; a->v = p->v; a->ks = p->k_scale; a->vs = p->v_scale;
+  a->B = b->n_requests; a->max_pages = b->max_pages; a->T = b->n_tokens;
+  a->table = b->page_table; a->lens = b->kv_len; a->starts = b->q_start;
+  return VLA_OK;
+}
+
+vla_status serve_buffers(const PageArgs& a, bool starts) {
+  auto al4 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; };
+  if (!a.k || !a.v || !al16(a.k) || !al16(a.v)) return fail(VLA_E_ARG, "k and v pages must be non-NULL and 16-byte aligned");
+  if (a.type >= VLA_KV_I8 && (!a.ks || !a.vs || !al16(a.ks) || !al16(a.vs)))
+    return fail(VLA_E_ARG, "8-bit pages need k_scale and v_scale, 16-byte aligned");
+  if (!a.table || !a.lens || (starts && !a.starts)) return fail(VLA_E_ARG, "page_table, kv_len or q_start is NULL");
+  if (!al4(a.table) || !al4(a.lens) || (starts && !al4(a.starts)))
+    return fail(VLA_E_ARG, "page_table, kv_len and q_start must be 4-byte aligned");
+  return VLA_OK;
+}
+
+// The attention's arguments that its plan depends on.
+vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, long long window, PagedAttnArgs* a) {
+  VLA_TRY(serve_sizes(pages, batch, &a->p));
+  if (n_heads < 1 || n_heads % a->p.G) return fail(VLA_E_SHAPE, "n_heads %d is not a multiple of %d K/V heads", n_heads, a->p.G);
+  a->H = n_heads;
+  a->R = n_heads / a->p.G;
+  if (a->R > 16) return fail(VLA_E_UNSUPPORTED, "more than 16 query heads per K/V head");
+  long long span = std::min<long long>(batch->max_len, (long long)batch->max_pages << a->p.lg);
+  if (window > 0) span = std::min(span, window + 1024);
+  a->window = window;
+  paged_attention_plan(*a, span);
+  if ((long long)a->slots * a->p.G * a->nsplit * 256 > kMaxThreads || (long long)a->p.T * a->H * 64 > kMaxThreads)
+    return fail(VLA_E_UNSUPPORTED, "too many tokens and heads for one call");
+  return VLA_OK;
+}
+
+}  // namespace
+
+vla_status vla_quantize_tokens(int32_t elem, const void* x, int32_t M, int32_t K, int64_t ldx, int8_t* q, int64_t ldq,
+                               float* r, void* stream) {
+  int es;
+  VLA_TRY(serve_elem(elem, &es));
+  if (M < 0 || K < 0) return fail(VLA_E_SHAPE, "negative dimension");
+  if (ldx < K || ldq < K) return fail(VLA_E_SHAPE, "ldx or ldq < K");
+  if (M == 0) return VLA_OK;
+  if ((long long)M * 256 > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many tokens for one call");
+  if (!r || (K > 0 && (!x || !q))) return fail(VLA_E_ARG, "NULL buffer");
+  if ((x && !al16(x)) || (q && !al16(q)) || !al16(r)) return fail(VLA_E_ARG, "buffers must be 16-byte aligned");
+  QuantTokArgs a{M, K, x, ldx, q, ldq, r};
+  HIP_TRY(launch_quantize_tokens(elem == VLA_T_F32, a, reinterpret_cast<hipStream_t>(stream)));
+  return VLA_OK;
+}
+
+vla_status vla_int8_gemm(const int8_t* q, int64_t ldq, const float* r, const int8_t* w, int64_t ldw, const float* w_scale,
+                         const float* bias, int32_t M, int32_t N, int32_t K, int32_t elem, void* y, int64_t ldy,
+                         void* stream) {
+  int es;
+  VLA_TRY(serve_elem(elem, &es));
+  if (M < 0 || N < 0 || K < 0) return fail(VLA_E_SHAPE, "negative dimension");
+  if (K % 16 || ldq % 16 || ldw % 16) return fail(VLA_E_SHAPE, "K, ldq and ldw must be multiples of 16");
+  if (K > 131056) return fail(VLA_E_SHAPE, "K too large for an exact int32 sum");
+  if (ldq < K || ldw < K || ldy < N) return fail(VLA_E_SHAPE, "a pitch is shorter than its row");
+  if (M == 0 || N == 0) return VLA_OK;
+  if (((M + 31LL) / 32 + 3) * ((N + 31LL) / 32 + 3) * 64 > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many outputs for one call");
+  if (!r || !w_scale || !y || (K > 0 && (!q || !w))) return fail(VLA_E_ARG, "NULL buffer");
+  if ((q && !al16(q)) || (w && !al16(w)) || !al16(r) || !al16(w_scale) || !al16(bias) || !al16(y))
+    return fail(VLA_E_ARG, "buffers must be 16-byte aligned");
+  Int8Args a{};
+  a.M = M; a.N = N; a.K = K; a.x = q; a.w = w; a.ldx = ldq; a.ldw = ldw; a.ldy = ldy;
+  a.r = r; a.wscale = w_scale; a.bias = bias; a.y = y; a.out_f32 = elem == VLA_T_F32;
+  HIP_TRY(launch_int8_gemm(a, reinterpret_cast<hipStream_t>(stream)));
+  return VLA_OK;
+}
+
+vla_status vla_kv_pages_write(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t elem, const void* k,
+                              const void* v, int64_t token_stride, int64_t head_stride, void* stream) {
+  int es;
+  VLA_TRY(serve_elem(elem, &es));
+  PageRowsArgs a{};
+  VLA_TRY(serve_sizes(pages, batch, &a.p));
+  if (token_stride < 0 || head_stride < 0 || token_stride * es % 16 || head_stride * es % 16)
+    return fail(VLA_E_SHAPE, "token_stride and head_stride must be multiples of 16 bytes");
+  if ((long long)a.p.T * 2 * a.p.G * a.p.hd / (16 / es) > kMaxThreads)
+    return fail(VLA_E_UNSUPPORTED, "too many tokens and heads for one call");
+  if (a.p.T == 0 || a.p.B == 0) return VLA_OK;
+  VLA_TRY(serve_buffers(a.p, true));
+  if (!k || !v || !al16(k) || !al16(v)) return fail(VLA_E_ARG, "k and v must be non-NULL and 16-byte aligned");
+  a.f32 = elem == VLA_T_F32; a.k = k; a.v = v; a.tstride = token_stride; a.hstride = head_stride;
+  HIP_TRY(launch_pages_write(a, reinterpret_cast<hipStream_t>(stream)));
+  return VLA_OK;
+}
+
+vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t rows, int32_t elem, void* k_out,
+                             void* v_out, void* stream) {
+  int es;
+  VLA_TRY(serve_elem(elem, &es));
+  PageRowsArgs a{};
+  VLA_TRY(serve_sizes(pages, batch, &a.p));
+  if (rows < 0) return fail(VLA_E_SHAPE, "negative dimension");
+  if ((long long)a.p.B * a.p.G * (a.p.hd / 16) * rows > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many rows for one call");
+  if (rows == 0 || a.p.B == 0) return VLA_OK;
+  VLA_TRY(serve_buffers(a.p, false));
+  if (!k_out || !v_out || !al16(k_out) || !al16(v_out)) return fail(VLA_E_ARG, "k_out and v_out must be non-NULL and 16-byte aligned");
+  a.f32 = elem == VLA_T_F32; a.ko = k_out; a.vo = v_out; a.rows = rows;
+  HIP_TRY(launch_pages_read(a, reinterpret_cast<hipStream_t>(stream)));
+  return VLA_OK;
+}
+
+size_t vla_paged_attention_workspace(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads) {
+  PagedAttnArgs a{};
+  if (paged_plan(pages, batch, n_heads, 0, &a) != VLA_OK) return (size_t)-1;
+  return paged_attention_bytes(a);
+}
+
+vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, int32_t elem,
+                               const void* q, int64_t ldq, void* o, int64_t ldo, float scale, int32_t causal,
+                               int32_t window, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  int es;
+  VLA_TRY(serve_elem(elem, &es));
+  if (window < 0) return fail(VLA_E_SHAPE, "negative window");
+  if (causal != 0 && causal != 1) return fail(VLA_E_ARG, "causal must be 0 or 1");
+  if (!std::isfinite(scale)) return fail(VLA_E_ARG, "scale must be finite");
+  PagedAttnArgs a{};
+  VLA_TRY(paged_plan(pages, batch, n_heads, window, &a));
+  if ((elem == VLA_T_F32) != (a.p.type == VLA_KV_F32))
+    return fail(VLA_E_UNSUPPORTED, "fp32 queries go with fp32 pages, bf16 queries with the other types");
+  const long long d = (long long)n_heads * a.p.hd;
+  if (ldq < d || ldo < d || ldq * es % 16 || ldo * es % 16)
+    return fail(VLA_E_SHAPE, "ldq and ldo must be at least n_heads * head_dim and multiples of 16 bytes");
+  if (a.p.T == 0 || a.p.B == 0) return VLA_OK;
+  VLA_TRY(serve_buffers(a.p, true));
+  if (!q || !o || !al16(q) || !al16(o) || !al16(lse)) return fail(VLA_E_ARG, "q and o must be non-NULL, q, o and lse 16-byte aligned");
+  const size_t need = vla_paged_attention_workspace(pages, batch, n_heads);
+  if (workspace_bytes < need) return fail(VLA_E_SHAPE, "workspace_bytes %zu < %zu", workspace_bytes, need);
+  if (need && (!workspace || !al16(workspace))) return fail(VLA_E_ARG, "workspace must be non-NULL and 16-byte aligned");
+  a.causal = causal; a.q = q; a.ldq = ldq; a.o = o; a.ldo = ldo; a.lse = lse; a.scale = scale;
+  a.part = static_cast<float*>(workspace);
+  a.stats = a.part + (size_t)a.nsplit * a.p.T * a.H * a.p.hd;
+  HIP_TRY(launch_paged_attention(a, reinterpret_cast<hipStream_t>(stream)));
+  return VLA_OK;
+}
+
 int32_t vla_profile_read(vla_model* m, vla_op_time* out, int32_t max_ops) {
   if (!m || !m->last_profiled) return -1;
   Plan* p = static_cast<Plan*>(m->last_profiled);

@@ -239,6 +239,67 @@ constexpr int kSkinnyRows = 128;   // row-major operands: most token rows of the
 inline int kstep(int et) { return et == 1 ? 32 : 16; }
 inline int kpad(int k) { return (k + 63) / 64 * 64; }
 
+// ---- 8-bit serving operators ----
+struct QuantTokArgs {
+  int M, K;
+  const void* x;           // [M][ldx] fp32 or bf16
+  long long ldx;
+  int8_t* q;               // [M][ldq]
+  long long ldq;
+  float* r;                // [M]
+};
+
+struct Int8Args {
+  int M, N, K;
+  const int8_t* x;         // [M][ldx]
+  const int8_t* w;         // [N][ldw]
+  long long ldx, ldw, ldy;
+  const float* r;          // [M] absmax of the token
+  const float* wscale;     // [N]
+  const float* bias;       // [N] or NULL
+  void* y;                 // [M][ldy]
+  int out_f32;
+  int m_tiles, n_tiles;    // set by the launcher
+};
+
+// Page pool and batch as the kernels see them (vla_kv_pages, vla_kv_batch).
+struct PageArgs {
+  int type;                // vla_kv_type
+  int n_pages, lg;         // page size 1 << lg
+  int G, hd;
+  void *k, *v;
+  float *ks, *vs;
+  int B, max_pages, T;
+  const int *table, *lens, *starts;
+};
+
+struct PageRowsArgs {      // write: rows in; read: rows out
+  PageArgs p;
+  int f32;                 // element type of the rows
+  const void *k, *v;       // write
+  long long tstride, hstride;
+  void *ko, *vo;           // read: [B][G][rows][hd]
+  int rows;
+};
+
+struct PagedAttnArgs {
+  PageArgs p;
+  int H, R;                // query heads, of them per K/V head
+  int causal;
+  long long window;        // 0: none
+  const void* q;
+  long long ldq;
+  void* o;
+  long long ldo;
+  float* lse;
+  float scale;
+  int slots;               // row tiles of all requests, at most (see paged_tile_of)
+  int nsplit;              // key splits
+  int chunk;               // keys per split (the last one takes the rest)
+  float* part;             // [nsplit][T][H][hd]: unnormalised output of each split (nsplit > 1)
+  float* stats;            // [nsplit][T][H][2]: its (max, sum)
+};
+
 // ---- launchers (each enqueues on `s`, returns hipError_t) ----
 // dst [ceil(N / 16)][ktiles][16][kstep] from row-major src [N][K], zeros past N and K
 hipError_t launch_retile(int et, void* dst, const void* src, int N, int K, int ktiles, hipStream_t s);
@@ -305,3 +366,13 @@ bool persist_supported(int d, int hd, int H, int G, int F, int n, int P, int A, 
 bool persist_resident(int d, int hd, int HT, int F);
 size_t persist_lds_bytes(int hd, int HT);
 hipError_t launch_persist(const PersistArgs& a, hipStream_t s);
+// 8-bit serving operators
+hipError_t launch_quantize_tokens(int f32, const QuantTokArgs& a, hipStream_t s);
+hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s);
+hipError_t launch_pages_write(const PageRowsArgs& a, hipStream_t s);
+hipError_t launch_pages_read(const PageRowsArgs& a, hipStream_t s);
+// Row tiles, splits and split length for these sizes (max_len: the host's
+// bound of the rows of a request; span: rows that a tile of queries may see).
+void paged_attention_plan(PagedAttnArgs& a, long long span);
+size_t paged_attention_bytes(const PagedAttnArgs& a);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s);

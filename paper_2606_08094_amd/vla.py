@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libvla.so")
 PATTERNS = {"self_cross": 0, "joint": 1, "alt": 2, "cross": 3}
 MLPS = {"gelu": 0, "geglu": 1, "swiglu": 2, "relu2glu": 3}
 WTYPES = {"f32": 0, "bf16": 1, "ternary": 2}
+ELEMS = {"f32": 0, "bf16": 1}
+KV_TYPES = {"f32": 0, "bf16": 1, "i8": 2, "e4m3": 3}
 STATUS = {0: "VLA_OK", 1: "VLA_E_ARG", 2: "VLA_E_SHAPE", 3: "VLA_E_UNSUPPORTED", 4: "VLA_E_NOMEM",
           5: "VLA_E_DEVICE", 6: "VLA_E_NONFINITE"}
 VLA_OPT_LOOP_MODE = 0
@@ -39,6 +41,8 @@ EXPORTS = ["vla_weight_count", "vla_model_create", "vla_model_destroy", "vla_mod
            "vla_test_gemm", "vla_test_attention", "vla_test_quantize_i8", "vla_test_quantize_bf16", "vla_test_ternary_linear",
            "vla_test_ternary_gemm", "vla_test_rope",
            "vla_test_adarms", "vla_test_time_cond", "vla_test_persist_trace",
+           "vla_quantize_tokens", "vla_int8_gemm", "vla_kv_pages_write", "vla_kv_pages_read", "vla_paged_attention",
+           "vla_paged_attention_workspace",
            "vla_backbone_weight_count", "vla_backbone_create", "vla_backbone_destroy", "vla_prefix_prefill"]
 
 
@@ -66,6 +70,16 @@ class VlaOpTime(ctypes.Structure):
                 ("bytes", ctypes.c_double), ("flops", ctypes.c_double), ("ms", ctypes.c_float)]
 
 
+class VlaKvPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "n_pages", "page_size", "n_kv_heads", "head_dim")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class VlaKvBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_requests", "max_pages", "n_tokens", "max_len")] + [
+        (n, ctypes.c_void_p) for n in ("page_table", "kv_len", "q_start")]
+
+
 _lib = None
 
 
@@ -77,7 +91,8 @@ def lib():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it with python -m paper_2606_08094_amd.build")
     L = ctypes.CDLL(LIB_PATH)
-    vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    pages, batch = ctypes.POINTER(VlaKvPages), ctypes.POINTER(VlaKvBatch)
     sig = {
         "vla_weight_count": (i32, [ctypes.POINTER(VlaConfig)]),
         "vla_model_create": (i32, [ctypes.POINTER(VlaConfig), ctypes.POINTER(vp), i32, ctypes.POINTER(vp)]),
@@ -103,6 +118,12 @@ def lib():
         "vla_test_ternary_gemm": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp,
                                         ctypes.POINTER(ctypes.c_float), vp]),
         "vla_test_persist_trace": (i32, [vp, ctypes.POINTER(ctypes.c_uint64), i32]),
+        "vla_quantize_tokens": (i32, [i32, vp, i32, i32, i64, vp, i64, vp, vp]),
+        "vla_int8_gemm": (i32, [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp]),
+        "vla_kv_pages_write": (i32, [pages, batch, i32, vp, vp, i64, i64, vp]),
+        "vla_kv_pages_read": (i32, [pages, batch, i32, i32, vp, vp, vp]),
+        "vla_paged_attention": (i32, [pages, batch, i32, i32, vp, i64, vp, i64, ctypes.c_float, i32, i32, vp, vp, sz, vp]),
+        "vla_paged_attention_workspace": (sz, [pages, batch, i32]),
         "vla_backbone_weight_count": (i32, [ctypes.POINTER(VlaBackboneConfig)]),
         "vla_backbone_create": (i32, [ctypes.POINTER(VlaBackboneConfig), ctypes.POINTER(vp), i32,
                                       ctypes.POINTER(vp)]),
@@ -301,6 +322,81 @@ def weight_count(cfg) -> int:
 
 def ternary_gemm(x, w_packed, M: int, N: int, K: int, acc_out, stream=None):
     _check(lib().vla_ternary_gemm(_ptr(x), _ptr(w_packed), M, N, K, _ptr(acc_out), _stream(stream)))
+
+
+# ---- 8-bit serving operators -------------------------------------------------
+
+def _launch(call, where, stream):
+    """call(stream handle), with the device of tensor `where` as the current
+    one: a stream of None is that device's current stream."""
+    import torch
+    index = getattr(getattr(where, "device", None), "index", None)
+    if index is None or index == torch.cuda.current_device():
+        return _check(call(_stream(stream)))
+    with torch.cuda.device(index):
+        return _check(call(_stream(stream)))
+
+
+def quantize_tokens(elem: int, x, M: int, K: int, ldx: int, q, ldq: int, r, stream=None):
+    """Per-token int8 codes q [M][ldq] and absolute maxima r [M] of x [M][ldx]
+    (elem: 0 fp32, 1 bf16)."""
+    _launch(lambda s: lib().vla_quantize_tokens(elem, _ptr(x), M, K, ldx, _ptr(q), ldq, _ptr(r), s), x, stream)
+
+
+def int8_gemm(q, ldq: int, r, w, ldw: int, w_scale, bias, M: int, N: int, K: int, elem: int, y, ldy: int, stream=None):
+    """y [M][ldy] = (q w^T) * (w_scale[n] * r[m] / 127) + bias: int8 codes q, r of
+    quantize_tokens, int8 weights w [N][ldw] with a scale per channel."""
+    _launch(lambda s: lib().vla_int8_gemm(_ptr(q), ldq, _ptr(r), _ptr(w), ldw, _ptr(w_scale), _ptr(bias), M, N, K, elem,
+                                          _ptr(y), ldy, s), q, stream)
+
+
+class KVPages:
+    """A pool of K/V pages in the caller's tensors: k, v [n_pages][n_kv_heads]
+    [page_size][head_dim] of `type` ("f32", "bf16", "i8", "e4m3"), and for the
+    8-bit types k_scale, v_scale [n_pages][n_kv_heads][page_size] fp32."""
+
+    def __init__(self, type: str, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k, v, k_scale=None,
+                 v_scale=None):
+        self.tensors = (k, v, k_scale, v_scale)   # the struct holds addresses only
+        self._c = VlaKvPages(KV_TYPES[type], n_pages, page_size, n_kv_heads, head_dim, _ptr(k), _ptr(v), _ptr(k_scale),
+                             _ptr(v_scale))
+
+
+class KVBatch:
+    """The requests of a call: int32 device tensors page_table [n_requests]
+    [max_pages], kv_len [n_requests] and q_start [n_requests + 1]."""
+
+    def __init__(self, n_requests: int, max_pages: int, n_tokens: int, max_len: int, page_table, kv_len, q_start=None):
+        self.tensors = (page_table, kv_len, q_start)
+        self._c = VlaKvBatch(n_requests, max_pages, n_tokens, max_len, _ptr(page_table), _ptr(kv_len), _ptr(q_start))
+
+
+def kv_pages_write(pages: KVPages, batch: KVBatch, elem: int, k, v, token_stride: int, head_stride: int, stream=None):
+    """The new tokens' keys and values into their pages, quantised as the pages are."""
+    _launch(lambda s: lib().vla_kv_pages_write(pages._c, batch._c, elem, _ptr(k), _ptr(v), token_stride, head_stride, s),
+            pages.tensors[0], stream)
+
+
+def kv_pages_read(pages: KVPages, batch: KVBatch, rows: int, elem: int, k_out, v_out, stream=None):
+    """The first `rows` rows of every request as k_out, v_out [n_requests][n_kv_heads][rows][head_dim]."""
+    _launch(lambda s: lib().vla_kv_pages_read(pages._c, batch._c, rows, elem, _ptr(k_out), _ptr(v_out), s),
+            pages.tensors[0], stream)
+
+
+def paged_attention_workspace(pages: KVPages, batch: KVBatch, n_heads: int) -> int:
+    n = lib().vla_paged_attention_workspace(pages._c, batch._c, n_heads)
+    if n == ctypes.c_size_t(-1).value:
+        raise VlaError(2, lib().vla_last_error().decode())
+    return n
+
+
+def paged_attention(pages: KVPages, batch: KVBatch, n_heads: int, elem: int, q, ldq: int, o, ldo: int, scale: float,
+                    causal: bool = False, window: int = 0, lse=None, workspace=None, workspace_bytes: int = 0,
+                    stream=None):
+    """Attention of the new tokens q [n_tokens][ldq] over the pages of their requests."""
+    _launch(lambda s: lib().vla_paged_attention(pages._c, batch._c, n_heads, elem, _ptr(q), ldq, _ptr(o), ldo,
+                                                float(scale), int(bool(causal)), int(window), _ptr(lse),
+                                                _ptr(workspace), workspace_bytes, s), pages.tensors[0], stream)
 
 
 # ---- test-only per-kernel entries (include/vla_test.h) ---------------------
