@@ -1732,7 +1732,7 @@ vla_status vla_int8_gemm(const int8_t* q, int64_t ldq, const float* r, const int
   if (K > 131056) return fail(VLA_E_SHAPE, "K too large for an exact int32 sum");
   if (ldq < K || ldw < K || ldy < N) return fail(VLA_E_SHAPE, "a pitch is shorter than its row");
   if (M == 0 || N == 0) return VLA_OK;
-  if (((M + 31LL) / 32 + 3) * ((N + 31LL) / 32 + 3) * 64 > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many outputs for one call");
+  if (((M + 63LL) / 64) * ((N + 63LL) / 64) > (1 << 22) || (N + 15LL) / 16 > (1 << 22)) return fail(VLA_E_UNSUPPORTED, "too many outputs for one call");
   if (!r || !w_scale || !y || (K > 0 && (!q || !w))) return fail(VLA_E_ARG, "NULL buffer");
   if ((q && !al16(q)) || (w && !al16(w)) || !al16(r) || !al16(w_scale) || !al16(bias) || !al16(y))
     return fail(VLA_E_ARG, "buffers must be 16-byte aligned");
