@@ -29,6 +29,10 @@ VLA_DEV float over_groups(float v, F f) {
 VLA_DEV float groups_max(float v) { return over_groups(v, [](float x, float y) { return fmaxf(x, y); }); }
 VLA_DEV float groups_sum(float v) { return over_groups(v, [](float x, float y) { return x + y; }); }
 
+// x / R and x % R for 0 <= x < 2^28 (rdiv = ceil(2^32 / R), R <= 16).
+VLA_DEV int by_r(const PagedAttnArgs& a, int x) { return (int)(((unsigned long long)(unsigned)x * a.rdiv) >> 32); }
+VLA_DEV int mod_r(const PagedAttnArgs& a, int x) { return x - by_r(a, x) * a.R; }
+
 // The tile of one workgroup.  Request b owns tile slots floor(starts[b] R / ROWS)
 // + b and up: the next request's begin no earlier than its ceil(n R / ROWS)
 // tiles end, and there are floor(T R / ROWS) + B slots in all, so the host
@@ -44,24 +48,30 @@ struct Tile {
 template <int ROWS>
 VLA_DEV bool paged_tile_of(const PagedAttnArgs& a, int slot, Tile& t) {
   const PageArgs& p = a.p;
-  auto first = [&](int b) { return (int)((long long)p.starts[b] * a.R / ROWS) + b; };
   const int lane = threadIdx.x & 63;
-  int cnt = 0;
-  for (int base = 0; base < p.B; base += 64) {
-    const int i = base + lane;
-    const unsigned long long in = __ballot(i < p.B && first(min(i, p.B - 1)) <= slot);
-    cnt += __popcll(in);
+  int found = -1, s0 = 0, s1 = 0, kv = 0, at = 0;
+  for (int base = 0; base < p.B; base += 64) {   // 64 requests at a time, all that is needed of them in one go
+    const int i = min(base + lane, p.B - 1);
+    const int si = p.starts[i], ei = p.starts[i + 1], li = p.lens[i];
+    const int fi = (int)((long long)si * a.R / ROWS) + i;
+    const unsigned long long in = __ballot(base + lane < p.B && fi <= slot);
+    if (in) {
+      const int l = __popcll(in) - 1;
+      found = base + l;
+      s0 = __builtin_amdgcn_readlane(si, l);
+      s1 = __builtin_amdgcn_readlane(ei, l);
+      kv = __builtin_amdgcn_readlane(li, l);
+      at = __builtin_amdgcn_readlane(fi, l);
+    }
     if (in != ~0ull) break;
   }
-  if (cnt == 0) return false;
-  t.b = cnt - 1;
-  t.s0 = p.starts[t.b];
-  const int s1 = p.starts[t.b + 1];
-  t.n = s1 - t.s0;
-  if (t.s0 < 0 || s1 > p.T || t.n <= 0) return false;
-  t.row0 = (slot - first(t.b)) * ROWS;
+  if (found < 0) return false;
+  t.b = found;
+  t.s0 = s0;
+  t.n = s1 - s0;
+  if (s0 < 0 || s1 > p.T || t.n <= 0) return false;
+  t.row0 = (slot - at) * ROWS;
   if (t.row0 < 0 || t.row0 >= t.n * a.R) return false;
-  const int kv = p.lens[t.b];
   const int cap = p.max_pages << p.lg;
   t.beyond = kv > cap;
   t.len = min(max(kv, 0), cap);
@@ -70,14 +80,35 @@ VLA_DEV bool paged_tile_of(const PagedAttnArgs& a, int slot, Tile& t) {
 }
 
 // Keys [lo, hi) that some row of the tile may see, of them those of one split
-// (none if lo >= hi); lo is rounded down to a block of 32.
+// (none if lo >= hi); lo is rounded down to a block of 32.  A request uses as
+// many splits as it has multiples of a.chunk keys, of equal length.
 VLA_DEV void tile_keys(const PagedAttnArgs& a, const Tile& t, int rows, int split, int& lo, int& hi) {
-  const int i0 = t.row0 / a.R, i1 = min(t.n - 1, (t.row0 + rows - 1) / a.R);
+  const int i0 = by_r(a, t.row0), i1 = min(t.n - 1, by_r(a, t.row0 + rows - 1));
   hi = a.causal ? min(t.len, t.pos0 + i1 + 1) : t.len;
   lo = a.window > 0 ? (int)max(0LL, (long long)t.pos0 + i0 - a.window + 1) : 0;
-  const long long base = (lo & ~31) + (long long)split * a.chunk;
-  if (split + 1 < a.nsplit) hi = (int)min((long long)hi, base + a.chunk);
-  lo = (int)min(base, 0x7fffff00LL);
+  lo &= ~31;
+  if (a.nsplit == 1) return;
+  const int span = max(hi - lo, 0);
+  const int ns = min((span + a.chunk - 1) / a.chunk, a.nsplit);
+  int each = ns > 0 ? (span + ns - 1) / ns : 0;
+  each = each > 64 ? (each + 127) & ~127 : (each + 31) & ~31;   // whole rounds of four waves, or one or two waves
+  if (split >= ns) {
+    hi = lo;
+    return;
+  }
+  lo += split * each;
+  if (split + 1 < ns) hi = min(hi, lo + each);
+}
+
+// A split without keys only says so: its output is not read.
+VLA_DEV bool empty_split(const PagedAttnArgs& a, const Tile& t, int rows, int g, int split, int lo, int hi) {
+  if (a.nsplit == 1 || lo < hi) return false;
+  const int rr = t.row0 + threadIdx.x;
+  if ((int)threadIdx.x < rows && rr < t.n * a.R) {
+    const size_t th = (size_t)(t.s0 + by_r(a, rr)) * a.H + g * a.R + mod_r(a, rr);
+    *reinterpret_cast<float2*>(a.stats + ((size_t)split * a.p.T * a.H + th) * 2) = make_float2(-INFINITY, t.beyond ? NAN : 0.0f);
+  }
+  return true;
 }
 
 // How a lane's share of a K or V row is laid out, by page type and head
@@ -137,6 +168,42 @@ VLA_DEV float v_value(const VecOf<B>& v, int e) {
 }
 VLA_DEV bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
 
+// Whether some value of a V vector is NaN or infinite; and the vector with
+// those set to zero.
+template <int TYPE, int B>
+VLA_DEV bool v_bad(const VecOf<B>& v) {
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < B / type_bytes(TYPE); ++e) bad |= not_finite(v_value<TYPE>(v, e));
+  return bad;
+}
+template <int TYPE, int B>
+VLA_DEV void v_clean(VecOf<B>& v) {
+#pragma unroll
+  for (int e = 0; e < B / type_bytes(TYPE); ++e)
+    if (not_finite(v_value<TYPE>(v, e))) {
+      if constexpr (TYPE == VLA_KV_F32) v.w[e] = 0;
+      else if constexpr (TYPE == VLA_KV_BF16) v.w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      else v.w[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+    }
+}
+// N (1, 2 or 4) neighbouring values.
+template <typename T, int N>
+VLA_DEV void put(T* d, const float* x) {
+  if constexpr (N == 1) *d = ElemTraits<T>::from_f(x[0]);
+  else if constexpr (sizeof(T) == 2 && N == 2) *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(x[0], x[1]);
+  else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+  else if constexpr (N == 2) *reinterpret_cast<float2*>(d) = make_float2(x[0], x[1]);
+  else *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
+}
+// One stored value (dimension dim of a row) as fp32, without its scale.
+template <int TYPE>
+VLA_DEV float stored(const void* row, int dim) {
+  if constexpr (TYPE == VLA_KV_F32) return reinterpret_cast<const float*>(row)[dim];
+  else if constexpr (TYPE == VLA_KV_BF16) return bf2f(reinterpret_cast<const bf16_t*>(row)[dim]);
+  else return code_f<TYPE>(reinterpret_cast<const uint8_t*>(row)[dim], 0);
+}
+
 // ---------------------------------------------------------------------------
 // paged_stream: a tile of 16 rows per workgroup, the keys of a split dealt to
 // four waves in blocks of 32.  K goes straight from memory into the MFMA A
@@ -145,8 +212,30 @@ VLA_DEV bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 
 // is a permutation of the lane's own registers; which of the head's dimensions
 // a row of an O^T tile stands for is free.  No LDS until the waves' results
 // are joined, no barrier among the loads.
+//
+// Bound by the cache's bytes.  A block's K and V are all in flight before the
+// first is used, and the page ids of the next one; the waves of a SIMD hide
+// each other's waits (a second block in flight per wave leaves room for half
+// the waves: 64 requests of up to 8192 rows of int8, 117 us instead of 113).
+// Loads have no branches: a key that does not exist is read from page 0 and
+// not used.
+// Workgroups per compute unit that the registers have to allow: as many as
+// they do without spilling.
 template <int TYPE, int HD>
-__global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
+constexpr int stream_occupancy() {
+  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : 2) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : HD == 128 ? 2 : 1) : (HD == 256 ? 2 : 4);
+}
+template <int TYPE, int HD>
+struct KvBlock {           // one lane's share of a block of 32 keys
+  using L = Lay<TYPE, HD>;
+  uint4 k[2][L::NK];
+  VecOf<L::VB> v[8][L::NH];
+  float4 ks[2], vs[2];     // 8-bit types: scales of keys 8 g4 .. 8 g4 + 7
+  int vpid;
+};
+
+template <int TYPE, int HD>
+__global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_stream(PagedAttnArgs a) {
   using L = Lay<TYPE, HD>;
   using E = std::conditional_t<L::F32, float, bf16_t>;
   constexpr int DT = L::DT, VE = L::VE, NH = L::NH, W = 4;
@@ -154,7 +243,7 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
   __shared__ float sm[W][16], sl[W][16];
 
   const PageArgs& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   const int units = a.slots * p.G * a.nsplit;
   int u = (int)(blockIdx.x % 8u) * (int)(gridDim.x / 8u) + (int)(blockIdx.x / 8u);
@@ -166,11 +255,50 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
   if (!paged_tile_of<16>(a, slot, t)) return;
   int k_lo, k_hi;
   tile_keys(a, t, 16, split, k_lo, k_hi);
+  if (empty_split(a, t, 16, g, split, k_lo, k_hi)) return;
+
+  // Pages of the keys whose K (group r16 / 4 of eight) and V (group g4) this lane loads.
+  const int* table = p.table + (size_t)t.b * p.max_pages;
+  const size_t pagerows = (size_t)1 << p.lg;
+  const int mask = (1 << p.lg) - 1;
+  auto pids = [&](int kb, int& kp, int& vp) {   // -1: past the split's keys
+    const int kk = kb + 8 * (r16 >> 2), vk = kb + 8 * g4;
+    kp = kk < k_hi ? table[kk >> p.lg] : -1;
+    vp = vk < k_hi ? table[vk >> p.lg] : -1;
+  };
+  auto load = [&](int kb, int kp, int vp, KvBlock<TYPE, HD>& x) {
+    const size_t kpid = (unsigned)kp < (unsigned)p.n_pages ? kp : 0;
+    x.vpid = (unsigned)vp < (unsigned)p.n_pages ? vp : -1;
+    const size_t krow = (kpid * p.G + g) * pagerows + ((kb + 8 * (r16 >> 2)) & mask) + (r16 & 3);
+    const size_t vrow = ((size_t)max(x.vpid, 0) * p.G + g) * pagerows + ((kb + 8 * g4) & mask);
+    const char* ka = reinterpret_cast<const char*>(p.k) + krow * (HD * L::ES) + 16 * g4;
+    const char* va = reinterpret_cast<const char*>(p.v) + vrow * (HD * L::ES) + r16 * L::VB;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int c = 0; c < L::NK; ++c) x.k[tt][c] = ldg16(ka + tt * 4 * (HD * L::ES) + 64 * c);
+    if constexpr (L::ES == 1) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x.ks[i] = __builtin_bit_cast(float4, ldg16(p.ks + vrow + 4 * i));
+        x.vs[i] = __builtin_bit_cast(float4, ldg16(p.vs + vrow + 4 * i));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh) x.v[j][hh] = ldgv<L::VB>(va + j * (HD * L::ES) + 16 * L::VB * hh);
+  };
+  constexpr int STEP = 32 * W;
+  const int kb0 = k_lo + 32 * wave;
+  KvBlock<TYPE, HD> buf;
+  int kp = -1, vp = -1;
+  pids(kb0, kp, vp);
 
   // this lane's row of the tile
   const int rr = t.row0 + r16;
   const bool rok = rr < t.n * a.R;
-  const int tok = rok ? rr / a.R : 0, h = g * a.R + (rok ? rr % a.R : 0);
+  const int tok = rok ? by_r(a, rr) : 0, h = g * a.R + (rok ? mod_r(a, rr) : 0);
   const int pos = t.pos0 + tok;
   // it sees keys [see_lo, see_hi)
   const int see_hi = rok ? (a.causal ? min(t.len, pos + 1) : t.len) : 0;
@@ -180,8 +308,8 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
 #pragma unroll
   for (int c = 0; c < L::QK; ++c) qf[c] = rok ? ldg16(qp + L::qdim(c, g4)) : make_uint4(0, 0, 0, 0);
   // every row of the tile sees every key in [all_lo, all_hi)
-  const int i1 = min(t.n - 1, (t.row0 + 15) / a.R);
-  const int all_hi = a.causal ? min(t.len, t.pos0 + t.row0 / a.R + 1) : t.len;
+  const int i1 = min(t.n - 1, by_r(a, t.row0 + 15));
+  const int all_hi = min(k_hi, a.causal ? min(t.len, t.pos0 + by_r(a, t.row0) + 1) : t.len);
   const int all_lo = a.window > 0 ? (int)max(0LL, (long long)t.pos0 + i1 - a.window + 1) : 0;
 
   f32x4 o[DT];
@@ -189,36 +317,11 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
   for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   float mrun = -INFINITY, lrun = 0.0f;
   const float sc = a.scale * kLog2e;
-  const size_t pagerows = (size_t)1 << p.lg;
-  const int mask = (1 << p.lg) - 1;
 
-  for (int kb = k_lo + 32 * wave; kb < k_hi; kb += 32 * W) {
-    // pages of the keys whose K (group r16 / 4) and V (group g4) this lane loads
-    const int kk0 = kb + 8 * (r16 >> 2), vk0 = kb + 8 * g4;
-    const int kpid = kk0 < k_hi ? page_of(p, t.b, kk0) : -1;
-    const int vpid = vk0 < k_hi ? page_of(p, t.b, vk0) : -1;
-    const size_t krow = ((size_t)max(kpid, 0) * p.G + g) * pagerows + (size_t)(kk0 & mask);
-    const size_t vrow = ((size_t)max(vpid, 0) * p.G + g) * pagerows + (size_t)(vk0 & mask);
-    uint4 kf[2][L::NK];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const int kr = 4 * tt + (r16 & 3);
-      const bool ok = kpid >= 0 && kk0 + kr < k_hi;
-      const char* kp = reinterpret_cast<const char*>(p.k) + (krow + kr) * (HD * L::ES) + 16 * g4;
-#pragma unroll
-      for (int c = 0; c < L::NK; ++c) kf[tt][c] = ok ? ldg16(kp + 64 * c) : make_uint4(0, 0, 0, 0);
-    }
-    VecOf<L::VB> vf[8][NH];
-    float ks[8], vs[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool ok = vpid >= 0 && vk0 + j < k_hi;
-      const char* vp = reinterpret_cast<const char*>(p.v) + (vrow + j) * (HD * L::ES) + r16 * L::VB;
-#pragma unroll
-      for (int hh = 0; hh < NH; ++hh) vf[j][hh] = ok ? ldgv<L::VB>(vp + 16 * L::VB * hh) : VecOf<L::VB>{};
-      ks[j] = L::ES == 1 && ok ? p.ks[vrow + j] : 1.0f;
-      vs[j] = L::ES == 1 && ok ? p.vs[vrow + j] : 1.0f;
-    }
+  auto block = [&](int kb, KvBlock<TYPE, HD>& x) {
+    const int vk0 = kb + 8 * g4;
+    // some row does not see some key, or a page is not there
+    const bool part = !(kb >= all_lo && kb + 32 <= all_hi) || __any(x.vpid < 0);
     f32x4 s[2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -226,85 +329,92 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
 #pragma unroll
       for (int c = 0; c < L::NK; ++c) {
         if constexpr (L::ES == 1) {
-          mma16(s[tt], codes_bf16<TYPE>(kf[tt][c].x, kf[tt][c].y), qf[2 * c], bf16_t());
-          mma16(s[tt], codes_bf16<TYPE>(kf[tt][c].z, kf[tt][c].w), qf[2 * c + 1], bf16_t());
+          mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].x, x.k[tt][c].y), qf[2 * c], bf16_t());
+          mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].z, x.k[tt][c].w), qf[2 * c + 1], bf16_t());
         } else {
-          mma16(s[tt], kf[tt][c], qf[c], E());
+          mma16(s[tt], x.k[tt][c], qf[c], E());
         }
       }
     }
-    // lane: keys vk0 + j of row r16.  A key on a page outside the pool is NaN
-    // where it is seen.
-    float x[8];
+    // lane: keys vk0 + j of row r16
+    const float ks[8] = {x.ks[0].x, x.ks[0].y, x.ks[0].z, x.ks[0].w, x.ks[1].x, x.ks[1].y, x.ks[1].z, x.ks[1].w};
+    const float vs[8] = {x.vs[0].x, x.vs[0].y, x.vs[0].z, x.vs[0].w, x.vs[1].x, x.vs[1].y, x.vs[1].z, x.vs[1].w};
+    float w[8];
     float bmax = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int key = vk0 + j;
-      const bool vis = key < see_hi && key >= see_lo && key < k_hi;
-      const float sv = s[j >> 2][j & 3] * (L::ES == 1 ? ks[j] * sc : sc);
-      x[j] = vis ? (vpid < 0 ? NAN : sv) : -INFINITY;
-      bmax = fmaxf(bmax, x[j]);
+      w[j] = s[j >> 2][j & 3] * (L::ES == 1 ? ks[j] * sc : sc);
+      if (part) {
+        const int key = vk0 + j;
+        // a key on a page outside the pool is NaN where it is seen
+        w[j] = key < see_hi && key >= see_lo && key < k_hi ? (x.vpid < 0 ? NAN : w[j]) : -INFINITY;
+      }
+      bmax = fmaxf(bmax, w[j]);
     }
     bmax = groups_max(bmax);
-    const float mnew = fmaxf(mrun, bmax);
+    // The reference moves only when a score exceeds it by more than 2^8: the
+    // exponentials stay below 256 and most blocks need no rescaling.
+    const bool move = bmax > mrun + 8.0f;
+    const float mnew = move ? bmax : mrun;
     const float mref = mnew == -INFINITY ? 0.0f : mnew;   // no visible key so far: weight 0
-    const float corr = __builtin_amdgcn_exp2f(mrun - mref);
+    const float corr = move ? __builtin_amdgcn_exp2f(mrun - mref) : 1.0f;
     float psum = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool hidden = x[j] == -INFINITY;
-      x[j] = __builtin_amdgcn_exp2f(x[j] - mref);
-      psum += x[j];
-      if constexpr (L::ES == 1) x[j] = hidden ? 0.0f : x[j] * vs[j];   // (the scale may be NaN)
+      const bool hidden = part && w[j] == -INFINITY;
+      w[j] = __builtin_amdgcn_exp2f(w[j] - mref);
+      psum += w[j];
+      if constexpr (L::ES == 1) w[j] = hidden ? 0.0f : w[j] * vs[j];   // (a hidden key's scale may be NaN)
     }
     lrun = lrun * corr + groups_sum(psum);
     mrun = mnew;
+    if (__any(move)) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= corr;
-
-    if constexpr (TYPE != VLA_KV_I8) {
-      // A NaN or an infinity in V must not reach the rows that do not see its
-      // key, and 0 times it would: where rows see different keys, such values
-      // are taken out of the product and added to the rows that see them.
-      if (!(kb >= all_lo && min(kb + 32, k_hi) <= all_hi)) {
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+    }
+    if (part) {
+      // Keys past the split or without a page are not what their registers hold.
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (x.vpid < 0 || vk0 + j >= k_hi) {
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh) x.v[j][hh] = VecOf<L::VB>{};
+        }
+      if constexpr (TYPE != VLA_KV_I8) {
+        // A NaN or an infinity in V must not reach the rows that do not see its
+        // key, and 0 times it would: such values are taken out of the product
+        // and added to the rows that see them.
         bool bad = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int hh = 0; hh < NH; ++hh)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) bad |= not_finite(v_value<TYPE>(vf[j][hh], e));
+          for (int hh = 0; hh < NH; ++hh) bad |= v_bad<TYPE>(x.v[j][hh]);
         if (__any(bad)) {
+          float* pw = &so[wave][0][0][0];   // [32 keys][16 rows] weights, this wave's own
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            pw[(8 * g4 + j) * 16 + r16] = w[j];
+#pragma unroll
+            for (int hh = 0; hh < NH; ++hh) v_clean<TYPE>(x.v[j][hh]);
+          }
+          __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the wave's own writes
+          __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-          for (int gk = 0; gk < 4; ++gk)
+          for (int kk = 0; kk < 32; ++kk) {
+            const int key = kb + kk;
+            const int pid = key < k_hi ? table[key >> p.lg] : -1;
+            if ((unsigned)pid >= (unsigned)p.n_pages) continue;
+            const char* row = reinterpret_cast<const char*>(p.v) + (((size_t)pid * p.G + g) * pagerows + (key & mask)) * (HD * L::ES);
+            const float pk = pw[kk * 16 + r16];
+            const bool vis = key < see_hi && key >= see_lo;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int key = kb + 8 * gk + j;
-              const float pk = __shfl(x[j], 16 * gk + r16, 64);
-              const bool vis = key < see_hi && key >= see_lo && key < k_hi;
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-              for (int hh = 0; hh < NH; ++hh)
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                  const float own = v_value<TYPE>(vf[j][hh], e);
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    const float val = __shfl(own, 16 * gk + 4 * g4 + i, 64);
-                    if (vis && not_finite(val)) o[hh * VE + e][i] += pk * val;
-                  }
-                }
-            }
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int hh = 0; hh < NH; ++hh)
-#pragma unroll
-              for (int e = 0; e < VE; ++e)
-                if (not_finite(v_value<TYPE>(vf[j][hh], e))) {
-                  if constexpr (TYPE == VLA_KV_F32) vf[j][hh].w[e] = 0;
-                  else if constexpr (TYPE == VLA_KV_BF16) vf[j][hh].w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                  else vf[j][hh].w[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-                }
+              for (int i = 0; i < 4; ++i) {
+                const float val = stored<TYPE>(row, d / VE * 16 * VE + (4 * g4 + i) * VE + d % VE);
+                if (vis && not_finite(val)) o[d][i] += pk * val;
+              }
+          }
         }
       }
     }
@@ -317,34 +427,43 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
         for (int e = 0; e < VE; ++e)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            o[hh * VE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[j][hh].w[e]), x[j], o[hh * VE + e], 0, 0, 0);
+            o[hh * VE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[j][hh].w[e]), w[j], o[hh * VE + e], 0, 0, 0);
     } else {
-      const uint4 pb = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+      const uint4 pb = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-          uint32_t w[4];
+          uint32_t vt[4];
 #pragma unroll
           for (int jj = 0; jj < 4; ++jj) {
             if constexpr (TYPE == VLA_KV_BF16)
-              w[jj] = __builtin_amdgcn_perm(vf[2 * jj + 1][hh].w[e >> 1], vf[2 * jj][hh].w[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+              vt[jj] = __builtin_amdgcn_perm(x.v[2 * jj + 1][hh].w[e >> 1], x.v[2 * jj][hh].w[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
             else
-              w[jj] = pack_bf16x2(v_value<TYPE>(vf[2 * jj][hh], e), v_value<TYPE>(vf[2 * jj + 1][hh], e));
+              vt[jj] = pack_bf16x2(v_value<TYPE>(x.v[2 * jj][hh], e), v_value<TYPE>(x.v[2 * jj + 1][hh], e));
           }
-          mma16(o[hh * VE + e], make_uint4(w[0], w[1], w[2], w[3]), pb, bf16_t());
+          mma16(o[hh * VE + e], make_uint4(vt[0], vt[1], vt[2], vt[3]), pb, bf16_t());
         }
     }
+  };
+
+  for (int kb = kb0; kb < k_hi; kb += STEP) {
+    load(kb, kp, vp, buf);
+    pids(kb + STEP, kp, vp);
+    block(kb, buf);
   }
 
-  // Join the waves: tile d, row 4 g4 + i, column r16 of each.
+  // Join the waves that had keys: tile d, row 4 g4 + i, column r16 of each.
+  const int nact = max(1, min(W, (k_hi - k_lo + 31) / 32));
   if (t.beyond) lrun = NAN;
   if (g4 == 0) {
     sm[wave][r16] = mrun;
     sl[wave][r16] = lrun;
   }
+  if (wave < nact) {
 #pragma unroll
-  for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(so[wave][d][lane]) = o[d];
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(so[wave][d][lane]) = o[d];
+  }
   __syncthreads();
   float mx = -INFINITY;
 #pragma unroll
@@ -364,54 +483,78 @@ __global__ __launch_bounds__(256) void paged_stream(PagedAttnArgs a) {
     else if (a.lse) a.lse[th] = (mx + __log2f(tot)) * kLn2;
   }
   const float inv = whole ? (tot == 0.0f ? 0.0f : 1.0f / tot) : 1.0f;
+  // Row 4 g4 + i of tile (hh, e) is dimension hh 16 VE + (4 g4 + i) VE + e: a
+  // wave's DW = DT / 4 tiles are DW neighbouring dimensions, for each i.
+  constexpr int DW = DT / W;
+  const int d0 = wave * DW, dim0 = d0 / VE * 16 * VE + d0 % VE;
+  f32x4 v[DW];
 #pragma unroll
-  for (int dd = 0; dd < DT / W; ++dd) {
-    const int d = wave * (DT / W) + dd;
-    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int d = 0; d < DW; ++d) {
+    v[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < W; ++w) v += *reinterpret_cast<const f32x4*>(so[w][d][lane]) * f[w];
-    v *= inv;
-    // rows 4 g4 + i of tile (hh, e): dimension hh 16 VE + (4 g4 + i) VE + e
-    const int hh = d / VE, e = d % VE;
+    for (int w = 0; w < W; ++w)
+      if (w < nact) v[d] += *reinterpret_cast<const f32x4*>(so[w][d0 + d][lane]) * f[w];
+    v[d] *= inv;
+  }
+  float* pd = a.part + ((size_t)split * p.T * a.H + th) * HD + dim0;
+  E* od = reinterpret_cast<E*>(a.o) + (size_t)(t.s0 + tok) * a.ldo + (size_t)h * HD + dim0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int dim = hh * 16 * VE + (4 * g4 + i) * VE + e;
-      if (!whole) a.part[((size_t)split * p.T * a.H + th) * HD + dim] = v[i];
-      else reinterpret_cast<E*>(a.o)[(size_t)(t.s0 + tok) * a.ldo + (size_t)h * HD + dim] = ElemTraits<E>::from_f(v[i]);
-    }
+  for (int i = 0; i < 4; ++i) {
+    float x[DW];
+#pragma unroll
+    for (int d = 0; d < DW; ++d) x[d] = v[d][i];
+    if (!whole) put<float, DW>(pd + (4 * g4 + i) * VE, x);
+    else put<E, DW>(od + (4 * g4 + i) * VE, x);
   }
 }
 
-// Joins the splits of one (token, head) per wave: o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-template <int F32>
+// Joins the splits of one (token, head) per wave: o = sum_s 2^(m_s - m) o_s /
+// sum_s 2^(m_s - m) l_s.  Lane s weighs split s; the outputs of a split that
+// saw no key are not read (they may not have been written).
+template <int F32, int HD>
 __global__ __launch_bounds__(256) void paged_join(PagedAttnArgs a) {
   using E = std::conditional_t<F32, float, bf16_t>;
+  constexpr int V = HD / 64;   // values per lane
   const PageArgs& p = a.p;
-  const long long th = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const long long th = (long long)blockIdx.x * 4 + wave;
   const long long all = (long long)p.T * a.H;
   if (th >= all) return;
   const int t = (int)(th / a.H), h = (int)(th - (long long)t * a.H);
+  const float2 st = lane < a.nsplit ? *reinterpret_cast<const float2*>(a.stats + ((size_t)lane * all + th) * 2)
+                                    : make_float2(-INFINITY, 0.0f);
   if (t < p.starts[0] || t >= p.starts[p.B]) return;   // padding
-  float mx = -INFINITY;
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float2 st = *reinterpret_cast<const float2*>(a.stats + ((size_t)s * all + th) * 2);
-    if (st.y != 0.0f) mx = fmaxf(mx, st.x);
-  }
+  const bool any = st.y != 0.0f;
+  const float mx = wave_max(any ? st.x : -INFINITY);
   const float mref = mx == -INFINITY ? 0.0f : mx;
-  float tot = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const int c = lane * (p.hd / 64);
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float2 st = *reinterpret_cast<const float2*>(a.stats + ((size_t)s * all + th) * 2);
-    if (st.y == 0.0f) continue;   // a split without keys
-    const float f = __builtin_amdgcn_exp2f(st.x - mref);
-    tot += st.y * f;
-    const float* src = a.part + ((size_t)s * all + th) * p.hd + c;
-    for (int i = 0; i < p.hd / 64; ++i) acc[i] += src[i] * f;
+  const float f = any ? __builtin_amdgcn_exp2f(st.x - mref) : 0.0f;
+  const float tot = wave_sum(any ? st.y * f : 0.0f);
+  const unsigned long long live = __ballot(any);
+  float acc[V] = {};
+  constexpr int U = 8;
+  for (int s0 = 0; s0 < a.nsplit; s0 += U) {
+    float v[U][V];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[j][i] = 0.0f;
+      if (s0 + j < 64 && (live >> (s0 + j) & 1)) {
+        const VecOf<4 * V> x = ldgv<4 * V>(a.part + ((size_t)(s0 + j) * all + th) * HD + lane * V);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j][i] = __uint_as_float(x.w[i]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(s0 + j, 63)));
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += v[j][i] * w;
+    }
   }
   const float inv = tot == 0.0f ? 0.0f : 1.0f / tot;
-  E* dst = reinterpret_cast<E*>(a.o) + (size_t)t * a.ldo + (size_t)h * p.hd + c;
-  for (int i = 0; i < p.hd / 64; ++i) dst[i] = ElemTraits<E>::from_f(acc[i] * inv);
+  E* dst = reinterpret_cast<E*>(a.o) + (size_t)t * a.ldo + (size_t)h * HD + lane * V;
+#pragma unroll
+  for (int i = 0; i < V; ++i) dst[i] = ElemTraits<E>::from_f(acc[i] * inv);
   if (lane == 0 && a.lse) a.lse[th] = (mx + __log2f(tot)) * kLn2;
 }
 
@@ -435,12 +578,17 @@ hipError_t stream_hd(const PagedAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 void paged_attention_plan(PagedAttnArgs& a, long long span) {
+  a.rdiv = ((1ull << 32) + a.R - 1) / a.R;
   a.slots = (int)((long long)a.p.T * a.R / 16) + a.p.B;
   const long long base = std::max(1LL, (long long)a.slots * a.p.G);
-  const long long want = (512 + base - 1) / base, most = std::max(1LL, (span + 127) / 128);
-  a.nsplit = (int)std::max(1LL, std::min({want, most, 64LL}));
-  a.chunk = (int)std::min<long long>(((span + a.nsplit - 1) / a.nsplit + 127) / 128 * 128, 1 << 30);
-  if (a.chunk < 128) a.chunk = 128;
+  // Key splits: about 1536 workgroups (64 requests of up to 8192 rows of int8:
+  // 118 us with 512, 103 with 1536, 116 with 4096), a wave's 32 keys at least:
+  // a CU takes in some 50 GB/s, so a short request is spread wide as well.  Up
+  // to 256 rows one workgroup is done before a second launch would be (72 rows
+  // of fp32: 7.0 us, 9.6 in three splits).
+  a.nsplit = span <= 256 ? 1 : (int)std::max(1LL, std::min({(1536 + base - 1) / base, (span + 31) / 32, 64LL}));
+  a.chunk = (int)((span + a.nsplit - 1) / a.nsplit + 31) & ~31;
+  if (a.chunk < 32) a.chunk = 32;
 }
 
 size_t paged_attention_bytes(const PagedAttnArgs& a) {
@@ -459,7 +607,14 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   }
   if (e != hipSuccess || a.nsplit == 1) return e;
   const long long rows = (long long)a.p.T * a.H;
-  if (a.p.type == VLA_KV_F32) hipLaunchKernelGGL(paged_join<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(paged_join<0>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if (a.p.type == VLA_KV_F32) {
+    if (a.p.hd == 64) hipLaunchKernelGGL((paged_join<1, 64>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join<1, 128>), grid, dim3(256), 0, s, a);
+  } else {
+    if (a.p.hd == 64) hipLaunchKernelGGL((paged_join<0, 64>), grid, dim3(256), 0, s, a);
+    else if (a.p.hd == 128) hipLaunchKernelGGL((paged_join<0, 128>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join<0, 256>), grid, dim3(256), 0, s, a);
+  }
   return hipGetLastError();
 }

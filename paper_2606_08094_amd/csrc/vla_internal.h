@@ -285,6 +285,7 @@ struct PageRowsArgs {      // write: rows in; read: rows out
 struct PagedAttnArgs {
   PageArgs p;
   int H, R;                // query heads, of them per K/V head
+  unsigned long long rdiv; // ceil(2^32 / R)
   int causal;
   long long window;        // 0: none
   const void* q;

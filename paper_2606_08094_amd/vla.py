@@ -326,28 +326,37 @@ def ternary_gemm(x, w_packed, M: int, N: int, K: int, acc_out, stream=None):
 
 # ---- 8-bit serving operators -------------------------------------------------
 
-def _launch(call, where, stream):
-    """call(stream handle), with the device of tensor `where` as the current
-    one: a stream of None is that device's current stream."""
+def _raw_stream(index: int) -> int:
+    """Handle of a device's current stream (through the call that makes no
+    Stream object, where this torch has it: 0.1 us instead of 2.7)."""
     import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
+
+
+def _launch(f, where, stream, *args):
+    """f(*args, stream handle), with the device of tensor `where` as the current
+    one; a stream of None is that device's current stream."""
+    import torch
+    now = torch.cuda.current_device()
     index = getattr(getattr(where, "device", None), "index", None)
-    if index is None or index == torch.cuda.current_device():
-        return _check(call(_stream(stream)))
+    if index is None or index == now:
+        return _check(f(*args, _raw_stream(now) if stream is None else _stream(stream)))
     with torch.cuda.device(index):
-        return _check(call(_stream(stream)))
+        return _check(f(*args, _raw_stream(index) if stream is None else _stream(stream)))
 
 
 def quantize_tokens(elem: int, x, M: int, K: int, ldx: int, q, ldq: int, r, stream=None):
     """Per-token int8 codes q [M][ldq] and absolute maxima r [M] of x [M][ldx]
     (elem: 0 fp32, 1 bf16)."""
-    _launch(lambda s: lib().vla_quantize_tokens(elem, _ptr(x), M, K, ldx, _ptr(q), ldq, _ptr(r), s), x, stream)
+    _launch(lib().vla_quantize_tokens, x, stream, elem, _ptr(x), M, K, ldx, _ptr(q), ldq, _ptr(r))
 
 
 def int8_gemm(q, ldq: int, r, w, ldw: int, w_scale, bias, M: int, N: int, K: int, elem: int, y, ldy: int, stream=None):
     """y [M][ldy] = (q w^T) * (w_scale[n] * r[m] / 127) + bias: int8 codes q, r of
     quantize_tokens, int8 weights w [N][ldw] with a scale per channel."""
-    _launch(lambda s: lib().vla_int8_gemm(_ptr(q), ldq, _ptr(r), _ptr(w), ldw, _ptr(w_scale), _ptr(bias), M, N, K, elem,
-                                          _ptr(y), ldy, s), q, stream)
+    _launch(lib().vla_int8_gemm, q, stream, _ptr(q), ldq, _ptr(r), _ptr(w), ldw, _ptr(w_scale), _ptr(bias), M, N, K, elem,
+            _ptr(y), ldy)
 
 
 class KVPages:
@@ -373,14 +382,13 @@ class KVBatch:
 
 def kv_pages_write(pages: KVPages, batch: KVBatch, elem: int, k, v, token_stride: int, head_stride: int, stream=None):
     """The new tokens' keys and values into their pages, quantised as the pages are."""
-    _launch(lambda s: lib().vla_kv_pages_write(pages._c, batch._c, elem, _ptr(k), _ptr(v), token_stride, head_stride, s),
-            pages.tensors[0], stream)
+    _launch(lib().vla_kv_pages_write, pages.tensors[0], stream, pages._c, batch._c, elem, _ptr(k), _ptr(v), token_stride,
+            head_stride)
 
 
 def kv_pages_read(pages: KVPages, batch: KVBatch, rows: int, elem: int, k_out, v_out, stream=None):
     """The first `rows` rows of every request as k_out, v_out [n_requests][n_kv_heads][rows][head_dim]."""
-    _launch(lambda s: lib().vla_kv_pages_read(pages._c, batch._c, rows, elem, _ptr(k_out), _ptr(v_out), s),
-            pages.tensors[0], stream)
+    _launch(lib().vla_kv_pages_read, pages.tensors[0], stream, pages._c, batch._c, rows, elem, _ptr(k_out), _ptr(v_out))
 
 
 def paged_attention_workspace(pages: KVPages, batch: KVBatch, n_heads: int) -> int:
@@ -394,9 +402,8 @@ def paged_attention(pages: KVPages, batch: KVBatch, n_heads: int, elem: int, q, 
                     causal: bool = False, window: int = 0, lse=None, workspace=None, workspace_bytes: int = 0,
                     stream=None):
     """Attention of the new tokens q [n_tokens][ldq] over the pages of their requests."""
-    _launch(lambda s: lib().vla_paged_attention(pages._c, batch._c, n_heads, elem, _ptr(q), ldq, _ptr(o), ldo,
-                                                float(scale), int(bool(causal)), int(window), _ptr(lse),
-                                                _ptr(workspace), workspace_bytes, s), pages.tensors[0], stream)
+    _launch(lib().vla_paged_attention, pages.tensors[0], stream, pages._c, batch._c, n_heads, elem, _ptr(q), ldq, _ptr(o),
+            ldo, float(scale), int(bool(causal)), int(window), _ptr(lse), _ptr(workspace), workspace_bytes)
 
 
 # ---- test-only per-kernel entries (include/vla_test.h) ---------------------
