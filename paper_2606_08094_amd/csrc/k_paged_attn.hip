@@ -33,6 +33,19 @@ VLA_DEV float groups_sum(float v) { return over_groups(v, [](float x, float y) {
 VLA_DEV int by_r(const PagedAttnArgs& a, int x) { return (int)(((unsigned long long)(unsigned)x * a.rdiv) >> 32); }
 VLA_DEV int mod_r(const PagedAttnArgs& a, int x) { return x - by_r(a, x) * a.R; }
 
+// The scores' factor (base 2) is kept positive, so that a maximum of scores can
+// be taken before it is applied; one that is not positive turns the scores
+// themselves.
+VLA_DEV float score_factor(const PagedAttnArgs& a) { return a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e; }
+template <int N>
+VLA_DEV void turn_scores(const PagedAttnArgs& a, float (&w)[N]) {
+  if (a.scale <= 0.0f) {
+    const float f = a.scale < 0.0f ? -1.0f : 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] *= f;
+  }
+}
+
 // The tile of one workgroup.  Request b owns tile slots floor(starts[b] R / ROWS)
 // + b and up: the next request's begin no earlier than its ceil(n R / ROWS)
 // tiles end, and there are floor(T R / ROWS) + B slots in all, so the host
@@ -152,9 +165,16 @@ VLA_DEV VecOf<B> ldgv(const void* p) {
   return r;
 }
 
-// Eight codes (two dwords) as a bf16 MFMA operand vector (exact).
+// Eight codes (two dwords) as a bf16 MFMA operand vector (exact; e4m3 two at a
+// time, with a scale of one).
+template <bool HI>
+VLA_DEV uint32_t e4m3_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, HI));
+}
 template <int TYPE>
 VLA_DEV uint4 codes_bf16(uint32_t lo, uint32_t hi) {
+  if constexpr (TYPE == VLA_KV_E4M3)
+    return make_uint4(e4m3_pair<false>(lo), e4m3_pair<true>(lo), e4m3_pair<false>(hi), e4m3_pair<true>(hi));
   return make_uint4(pack_bf16x2(code_f<TYPE>(lo, 0), code_f<TYPE>(lo, 1)), pack_bf16x2(code_f<TYPE>(lo, 2), code_f<TYPE>(lo, 3)),
                     pack_bf16x2(code_f<TYPE>(hi, 0), code_f<TYPE>(hi, 1)), pack_bf16x2(code_f<TYPE>(hi, 2), code_f<TYPE>(hi, 3)));
 }
@@ -204,6 +224,29 @@ VLA_DEV float stored(const void* row, int dim) {
   else return code_f<TYPE>(reinterpret_cast<const uint8_t*>(row)[dim], 0);
 }
 
+// Adds the NaNs and infinities among the V values of keys [k0, k1) to the
+// outputs of the row that sees them ([see_lo, see_hi)); o[d][i] is dimension
+// dim(d, i).  The weights are positive, and such a sum is what it is whatever
+// they are.
+template <int TYPE, int HD, int DT, typename F>
+VLA_DEV void add_not_finite(const PageArgs& p, const int* table, int g, int k0, int k1, int see_lo, int see_hi, f32x4 (&o)[DT], F dim) {
+#pragma unroll 1
+  for (int key = k0; key < k1; ++key) {
+    const int pid = table[key >> p.lg];
+    if ((unsigned)pid >= (unsigned)p.n_pages) continue;
+    const size_t at = (((size_t)pid * p.G + g) << p.lg) + (key & ((1 << p.lg) - 1));
+    const char* row = reinterpret_cast<const char*>(p.v) + at * (HD * type_bytes(TYPE));
+    const bool vis = key < see_hi && key >= see_lo;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float val = stored<TYPE>(row, dim(d, i));
+        if (vis && not_finite(val)) o[d][i] += val;
+      }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // paged_stream: a tile of 16 rows per workgroup, the keys of a split dealt to
 // four waves in blocks of 32.  K goes straight from memory into the MFMA A
@@ -223,7 +266,7 @@ VLA_DEV float stored(const void* row, int dim) {
 // they do without spilling.
 template <int TYPE, int HD>
 constexpr int stream_occupancy() {
-  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : 2) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : HD == 128 ? 2 : 1) : (HD == 256 ? 2 : 4);
+  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : 2) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : HD == 128 ? 3 : 1) : (HD == 256 ? 2 : HD == 128 ? 3 : 4);
 }
 template <int TYPE, int HD>
 struct KvBlock {           // one lane's share of a block of 32 keys
@@ -316,62 +359,77 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   float mrun = -INFINITY, lrun = 0.0f;
-  const float sc = a.scale * kLog2e;
+  bool rare = false;   // V values that are not finite were taken out of a product
+  const float sc = score_factor(a);
 
   auto block = [&](int kb, KvBlock<TYPE, HD>& x) {
     const int vk0 = kb + 8 * g4;
     // some row does not see some key, or a page is not there
     const bool part = !(kb >= all_lo && kb + 32 <= all_hi) || __any(x.vpid < 0);
-    f32x4 s[2];
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      s[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < L::NK; ++c) {
+      if constexpr (L::ES == 1) {
 #pragma unroll
-      for (int c = 0; c < L::NK; ++c) {
-        if constexpr (L::ES == 1) {
-          mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].x, x.k[tt][c].y), qf[2 * c], bf16_t());
-          mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].z, x.k[tt][c].w), qf[2 * c + 1], bf16_t());
-        } else {
-          mma16(s[tt], x.k[tt][c], qf[c], E());
-        }
+        for (int tt = 0; tt < 2; ++tt) mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].x, x.k[tt][c].y), qf[2 * c], bf16_t());
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) mma16(s[tt], codes_bf16<TYPE>(x.k[tt][c].z, x.k[tt][c].w), qf[2 * c + 1], bf16_t());
+      } else {
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) mma16(s[tt], x.k[tt][c], qf[c], E());
       }
     }
     // lane: keys vk0 + j of row r16
     const float ks[8] = {x.ks[0].x, x.ks[0].y, x.ks[0].z, x.ks[0].w, x.ks[1].x, x.ks[1].y, x.ks[1].z, x.ks[1].w};
     const float vs[8] = {x.vs[0].x, x.vs[0].y, x.vs[0].z, x.vs[0].w, x.vs[1].x, x.vs[1].y, x.vs[1].z, x.vs[1].w};
     float w[8];
-    float bmax = -INFINITY;
+    unsigned hid = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = s[j >> 2][j & 3] * (L::ES == 1 ? ks[j] * sc : sc);
-      if (part) {
+    for (int j = 0; j < 8; ++j) w[j] = L::ES == 1 ? s[j >> 2][j & 3] * ks[j] : s[j >> 2][j & 3];
+    turn_scores(a, w);
+    if (part) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
         const int key = vk0 + j;
+        const bool vis = key < see_hi && key >= see_lo && key < k_hi;
         // a key on a page outside the pool is NaN where it is seen
-        w[j] = key < see_hi && key >= see_lo && key < k_hi ? (x.vpid < 0 ? NAN : w[j]) : -INFINITY;
+        w[j] = vis ? (x.vpid < 0 ? NAN : w[j]) : -INFINITY;
+        hid |= vis ? 0u : 1u << j;
       }
-      bmax = fmaxf(bmax, w[j]);
     }
-    bmax = groups_max(bmax);
-    // The reference moves only when a score exceeds it by more than 2^8: the
-    // exponentials stay below 256 and most blocks need no rescaling.
-    const bool move = bmax > mrun + 8.0f;
-    const float mnew = move ? bmax : mrun;
-    const float mref = mnew == -INFINITY ? 0.0f : mnew;   // no visible key so far: weight 0
-    const float corr = move ? __builtin_amdgcn_exp2f(mrun - mref) : 1.0f;
-    float psum = 0.0f;
+    float bmax = w[0];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool hidden = part && w[j] == -INFINITY;
-      w[j] = __builtin_amdgcn_exp2f(w[j] - mref);
-      psum += w[j];
-      if constexpr (L::ES == 1) w[j] = hidden ? 0.0f : w[j] * vs[j];   // (a hidden key's scale may be NaN)
-    }
-    lrun = lrun * corr + groups_sum(psum);
-    mrun = mnew;
-    if (__any(move)) {
+    for (int j = 1; j < 8; ++j) bmax = fmaxf(bmax, w[j]);
+    bmax *= sc;
+    // The reference moves only when a score exceeds it by more than 2^8: the
+    // exponentials stay below 256, most blocks need no rescaling, and until
+    // then no lane needs the others' maximum.
+    if (__any(bmax > mrun + 8.0f)) {
+      bmax = groups_max(bmax);
+      const bool move = bmax > mrun + 8.0f;
+      const float mnew = move ? bmax : mrun;
+      const float corr = move ? __builtin_amdgcn_exp2f(mrun - mnew) : 1.0f;
+      lrun *= corr;
+      mrun = mnew;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= corr;
     }
+    const float mref = mrun == -INFINITY ? 0.0f : mrun;   // no visible key so far: weight 0
+    float psum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      w[j] = __builtin_amdgcn_exp2f(fmaf(w[j], sc, -mref));
+      psum += w[j];
+    }
+    if constexpr (L::ES == 1) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] *= vs[j];
+      if (part) {   // a hidden key's scale may be NaN
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = hid >> j & 1 ? 0.0f : w[j];
+      }
+    }
+    lrun += psum;   // this lane's keys
     if (part) {
       // Keys past the split or without a page are not what their registers hold.
 #pragma unroll
@@ -383,38 +441,18 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
       if constexpr (TYPE != VLA_KV_I8) {
         // A NaN or an infinity in V must not reach the rows that do not see its
         // key, and 0 times it would: such values are taken out of the product
-        // and added to the rows that see them.
+        // and added to the rows that see them at the end (see add_not_finite).
         bool bad = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
           for (int hh = 0; hh < NH; ++hh) bad |= v_bad<TYPE>(x.v[j][hh]);
         if (__any(bad)) {
-          float* pw = &so[wave][0][0][0];   // [32 keys][16 rows] weights, this wave's own
+          rare = true;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            pw[(8 * g4 + j) * 16 + r16] = w[j];
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int hh = 0; hh < NH; ++hh) v_clean<TYPE>(x.v[j][hh]);
-          }
-          __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the wave's own writes
-          __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-          for (int kk = 0; kk < 32; ++kk) {
-            const int key = kb + kk;
-            const int pid = key < k_hi ? table[key >> p.lg] : -1;
-            if ((unsigned)pid >= (unsigned)p.n_pages) continue;
-            const char* row = reinterpret_cast<const char*>(p.v) + (((size_t)pid * p.G + g) * pagerows + (key & mask)) * (HD * L::ES);
-            const float pk = pw[kk * 16 + r16];
-            const bool vis = key < see_hi && key >= see_lo;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float val = stored<TYPE>(row, d / VE * 16 * VE + (4 * g4 + i) * VE + d % VE);
-                if (vis && not_finite(val)) o[d][i] += pk * val;
-              }
-          }
         }
       }
     }
@@ -453,9 +491,18 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
     block(kb, buf);
   }
 
+  if constexpr (TYPE != VLA_KV_I8) {
+    if (rare) {
+      for (int kb = kb0; kb < k_hi; kb += STEP)
+        if (!(kb >= all_lo && kb + 32 <= all_hi))
+          add_not_finite<TYPE, HD>(p, table, g, kb, min(kb + 32, k_hi), see_lo, see_hi, o,
+                                   [&](int d, int i) { return d / VE * 16 * VE + (4 * g4 + i) * VE + d % VE; });
+    }
+  }
+
   // Join the waves that had keys: tile d, row 4 g4 + i, column r16 of each.
   const int nact = max(1, min(W, (k_hi - k_lo + 31) / 32));
-  if (t.beyond) lrun = NAN;
+  lrun = t.beyond ? NAN : groups_sum(lrun);
   if (g4 == 0) {
     sm[wave][r16] = mrun;
     sl[wave][r16] = lrun;
@@ -505,6 +552,368 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
     for (int d = 0; d < DW; ++d) x[d] = v[d][i];
     if (!whole) put<float, DW>(pd + (4 * g4 + i) * VE, x);
     else put<E, DW>(od + (4 * g4 + i) * VE, x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// paged_tile: many rows per request (prompts, action chunks).  A workgroup of
+// NW waves takes 16 RS NW rows, RS subtiles of 16 per wave, and walks its keys
+// in blocks of 64 that are staged in LDS as bf16 (8-bit codes are widened once
+// for all rows) and serve every row:
+//   K [64 keys][HD]  16-byte chunk c of key k at slot c ^ kswz(k)
+//   V [64 keys][HD]  16-byte chunk c of key k at slot c ^ vswz(k)
+// kswz gives the eight keys of one bank cycle of a score operand eight slots.
+// V^T operands come from ds_read_b64_tr_b16: within 16 lanes, lane i receives
+// element i % 4 of the 8-byte blocks addressed by lanes i / 4, i / 4 + 4, + 8
+// and + 12, so lane p of group g addresses key 8 g + p / 4 (+ 4 for the second
+// read) at dimensions 16 d + 4 (p % 4) and gets four consecutive keys of
+// dimension 16 d + p; vswz puts the four keys of a read in disjoint banks.
+// An operand from LDS feeds RS MFMAs.  The next block's rows are on their way
+// in registers, and the page ids of the one after that, while a block is
+// worked on; LDS is double-buffered, one barrier per block.
+VLA_DEV uint4 pick(bool c, const uint4& x, const uint4& y) {   // (by dwords: a select of structs goes through memory)
+  return make_uint4(c ? x.x : y.x, c ? x.y : y.y, c ? x.z : y.z, c ? x.w : y.w);
+}
+VLA_DEV int kswz(int k) { return (k & 3) | ((k >> 1) & 4); }
+VLA_DEV int vswz(int k) { return 2 * (k & 3); }
+
+constexpr int TKB = 64;   // keys per block
+
+template <int TYPE, int HD, int RS, int NW>
+struct TileShape {
+  static constexpr int ROWS = 16 * RS * NW, THR = 64 * NW;
+  static constexpr int ES = type_bytes(TYPE);
+  static constexpr int VPR = HD * ES / 16;            // 16-byte vectors of a stored row
+  static constexpr int LD = TKB * VPR / THR;          // of them per thread and block (K; V the same)
+  static constexpr int KPW = 64 / VPR, KPL = THR / VPR;   // keys of a wave's load, keys of all waves' load
+  static constexpr int CPR = HD / 8;                  // 16-byte chunks of a staged row
+  static constexpr int BUF = 2 * TKB * CPR;           // chunks per buffer: K, then V
+  static_assert(LD * THR == TKB * VPR && KPW <= 16, "staging");
+};
+
+template <int TYPE, int HD, int RS, int NW, int OCC>
+__global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
+  using S = TileShape<TYPE, HD, RS, NW>;
+  constexpr int LD = S::LD, CPR = S::CPR, NQV = HD / 32, DT = HD / 16, ES = S::ES;
+  __shared__ uint4 st[2][S::BUF];
+  __shared__ __align__(16) float scl[2][2][TKB];   // 8-bit types: scales of the block's keys, K and V
+  __shared__ int rare;                         // V values that are not finite were taken out of a product
+
+  const PageArgs& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const int units = a.slots * p.G * a.nsplit;
+  int u = (int)(blockIdx.x % 8u) * (int)(gridDim.x / 8u) + (int)(blockIdx.x / 8u);
+  if (u >= units) return;
+  const int slot = u % a.slots;
+  u /= a.slots;
+  const int split = u % a.nsplit, g = u / a.nsplit;
+  Tile t;
+  if (!paged_tile_of<S::ROWS>(a, slot, t)) return;
+  int k_lo, k_hi;
+  tile_keys(a, t, S::ROWS, split, k_lo, k_hi);
+  if (empty_split(a, t, S::ROWS, g, split, k_lo, k_hi)) return;
+
+  const int* table = p.table + (size_t)t.b * p.max_pages;
+  const size_t pagerows = (size_t)1 << p.lg;
+  const int mask = (1 << p.lg) - 1;
+  const float sc = score_factor(a);
+  // rows of the tile that see every key in [all_lo, all_hi): of tokens i0 .. i1
+  auto all_of = [&](int row, int rows, int& lo, int& hi) {
+    const int i0 = by_r(a, row), i1 = min(t.n - 1, by_r(a, row + rows - 1));
+    hi = a.causal ? min(t.len, t.pos0 + i0 + 1) : t.len;
+    lo = a.window > 0 ? (int)max(0LL, (long long)t.pos0 + i1 - a.window + 1) : 0;
+  };
+  int tile_lo, tile_hi;   // every row of the tile sees these
+  all_of(t.row0, S::ROWS, tile_lo, tile_hi);
+
+  // Pages of a block's four groups of 16 keys, group lane / 16 in each lane: -1
+  // past the split, -2 outside the pool.
+  auto pages = [&](int kb) {
+    const int key = kb + 16 * g4;
+    int pid = -1;
+    if (key < k_hi) {
+      pid = table[key >> p.lg];
+      if ((unsigned)pid >= (unsigned)p.n_pages) pid = -2;
+    }
+    return pid;
+  };
+  // The keys that load i of this wave brings are of one group.
+  const int key0 = wave * S::KPW, lkey = lane / S::VPR, lvec = lane % S::VPR;
+  auto page_of_load = [&](int pg, int i) { return __builtin_amdgcn_readlane(pg, (key0 + S::KPL * i) & 48); };
+  const unsigned pstride = (unsigned)p.G << p.lg;   // rows of a page (of all heads); times the row's bytes below 2^29
+  const char* kbase = reinterpret_cast<const char*>(p.k) + ((size_t)g << p.lg) * (HD * ES) + lane * 16;
+  const char* vbase = reinterpret_cast<const char*>(p.v) + ((size_t)g << p.lg) * (HD * ES) + lane * 16;
+  uint4 kr[LD], vr[LD];
+  float sreg = 0.0f;           // one scale of the block in the registers: thread key (K) or 64 + key (V)
+  auto load = [&](int kb, int pg) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int key = kb + key0 + S::KPL * i;
+      const size_t off = (size_t)(unsigned)max(page_of_load(pg, i), 0) * (pstride * (HD * ES)) + (unsigned)(key & mask) * (HD * ES);
+      kr[i] = ldg16(kbase + off);
+      vr[i] = ldg16(vbase + off);
+    }
+    if constexpr (ES == 1) {
+      if (wave < 2) {          // lane: key kb + lane, of page group lane / 16
+        const size_t row = ((size_t)max(pg, 0) * p.G + g) * pagerows + ((kb + lane) & mask);
+        sreg = (wave == 0 ? p.ks : p.vs)[row];
+        if (wave == 0) sreg = pg == -2 ? NAN : sreg;
+        else if (pg < 0) sreg = 0.0f;
+      }
+    }
+  };
+  // registers -> LDS buffer b
+  auto stage = [&](int kb, int b, int pg) {
+    // some row does not see some key, or a page is not there
+    const bool part = !(kb >= tile_lo && kb + TKB <= min(tile_hi, k_hi)) || __any(pg < 0);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int k = key0 + S::KPL * i + lkey;    // key of the block
+      uint4 v = vr[i];
+      if (part && (page_of_load(pg, i) < 0 || kb + k >= k_hi)) v = make_uint4(0, 0, 0, 0);   // not what the registers hold
+      if constexpr (TYPE != VLA_KV_I8) {
+        if (part) {
+          VecOf<16> x{{v.x, v.y, v.z, v.w}};
+          if (v_bad<TYPE>(x)) {
+            bad = true;
+            v_clean<TYPE>(x);
+            v = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+          }
+        }
+      }
+      uint4* kl = st[b] + k * CPR;
+      uint4* vl = st[b] + (TKB + k) * CPR;
+      if constexpr (ES == 1) {
+        // Two chunks each; lanes 4 .. 7 of eight begin with the second, so that
+        // the eight write eight different slots (of K rows of 64 the two keys
+        // in them differ in their swizzle's lowest bit already).
+        const int swv = lane >> 2 & 1, swk = HD == 64 ? 0 : swv;
+        const uint4 k0 = codes_bf16<TYPE>(kr[i].x, kr[i].y), k1 = codes_bf16<TYPE>(kr[i].z, kr[i].w);
+        const uint4 v0 = codes_bf16<TYPE>(v.x, v.y), v1 = codes_bf16<TYPE>(v.z, v.w);
+        kl[(2 * lvec + swk) ^ kswz(k)] = pick(swk, k1, k0);
+        kl[(2 * lvec + 1 - swk) ^ kswz(k)] = pick(swk, k0, k1);
+        vl[(2 * lvec + swv) ^ vswz(k)] = pick(swv, v1, v0);
+        vl[(2 * lvec + 1 - swv) ^ vswz(k)] = pick(swv, v0, v1);
+      } else {
+        kl[lvec ^ kswz(k)] = kr[i];
+        vl[lvec ^ vswz(k)] = v;
+      }
+    }
+    if constexpr (ES == 1) {
+      if (wave < 2) scl[b][wave][lane] = sreg;
+    }
+    if constexpr (TYPE != VLA_KV_I8) {
+      if (part && __any(bad) && lane == 0) rare = 1;
+    }
+  };
+
+  // this lane's rows
+  int see_lo[RS], see_hi[RS];
+  uint4 qf[RS][NQV];
+  const int wrow = t.row0 + wave * 16 * RS;
+  int wave_lo, wave_hi;   // every row of the wave sees these
+  all_of(wrow, 16 * RS, wave_lo, wave_hi);
+  // and none sees a key from here on, or before
+  const int w1 = min(t.n - 1, by_r(a, wrow + 16 * RS - 1)), w0 = by_r(a, wrow);
+  const int none_hi = wrow >= t.n * a.R ? 0 : a.causal ? min(t.len, t.pos0 + w1 + 1) : t.len;
+  const int none_lo = a.window > 0 ? (int)max(0LL, (long long)t.pos0 + w0 - a.window + 1) : 0;
+#pragma unroll
+  for (int s = 0; s < RS; ++s) {
+    const int rr = wrow + 16 * s + r16;
+    const bool rok = rr < t.n * a.R;
+    const int tok = rok ? by_r(a, rr) : 0, h = g * a.R + (rok ? mod_r(a, rr) : 0);
+    see_hi[s] = rok ? (a.causal ? min(t.len, t.pos0 + tok + 1) : t.len) : 0;
+    see_lo[s] = a.window > 0 ? (int)max(0LL, (long long)t.pos0 + tok - a.window + 1) : 0;
+    const bf16_t* qp = reinterpret_cast<const bf16_t*>(a.q) + (size_t)(t.s0 + tok) * a.ldq + (size_t)h * HD + g4 * (HD / 4);
+#pragma unroll
+    for (int c = 0; c < NQV; ++c) qf[s][c] = rok ? ldg16(qp + 8 * c) : make_uint4(0, 0, 0, 0);
+  }
+  // LDS operand places of this lane: score row r16 is key 32 kk + 4 tt + 8 (r16 / 4) + r16 % 4
+  const int kkey = 8 * (r16 >> 2) + (r16 & 3), kf = kswz(kkey);
+  int vb[4];   // byte offset of the V^T reads of dim tiles d with d % 4 == q; tile d adds 128 (d / 4)
+  {
+    const int q4 = r16 >> 2, rowb = (8 * g4 + q4) * HD * 2;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) vb[q] = rowb + (((2 * q + ((r16 & 3) >> 1)) ^ (2 * q4)) * 16) + (r16 & 1) * 8;
+  }
+
+  f32x4 o[RS][DT];
+  float mrun[RS], lrun[RS];
+#pragma unroll
+  for (int s = 0; s < RS; ++s) {
+    mrun[s] = -INFINITY;
+    lrun[s] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[s][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // this lane's keys' scales (32 kk + 8 g4 + j of the block)
+  auto scales = [&](const float* from, float (&to)[16]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 v = *reinterpret_cast<const float4*>(from + 32 * (q >> 1) + 8 * g4 + 4 * (q & 1));
+      to[4 * q] = v.x; to[4 * q + 1] = v.y; to[4 * q + 2] = v.z; to[4 * q + 3] = v.w;
+    }
+  };
+  auto block = [&](int kb, int b, int pg) {
+    if (kb >= none_hi || kb + TKB <= none_lo) return;
+    const uint4* kl = st[b];
+    const unsigned char* vl = reinterpret_cast<const unsigned char*>(st[b] + TKB * CPR);
+    f32x4 s[RS][2][2];
+#pragma unroll
+    for (int r = 0; r < RS; ++r)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) s[r][kk][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NQV; ++c)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          const uint4 kv = kl[(kkey + 32 * kk + 4 * tt) * CPR + ((g4 * NQV + c) ^ kf)];
+#pragma unroll
+          for (int r = 0; r < RS; ++r) mma16(s[r][kk][tt], kv, qf[r][c], bf16_t());
+        }
+    // some row of the wave does not see some key, or a page is not there
+    const bool part = !(kb >= wave_lo && kb + TKB <= min(wave_hi, k_hi)) || __any(pg < 0);
+    uint4 pb[RS][2];
+    float w[RS][16], kv[16];
+    unsigned hid[RS];
+    if constexpr (ES == 1) scales(scl[b][0], kv);
+#pragma unroll
+    for (int r = 0; r < RS; ++r)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[r][i] = ES == 1 ? s[r][i >> 3][i >> 2 & 1][i & 3] * kv[i] : s[r][i >> 3][i >> 2 & 1][i & 3];
+#pragma unroll
+    for (int r = 0; r < RS; ++r) turn_scores(a, w[r]);
+    if (part) {
+      int gp[2];      // pages of this lane's keys
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) gp[kk] = __shfl(pg, 16 * (2 * kk + (g4 >> 1)), 64);
+#pragma unroll
+      for (int r = 0; r < RS; ++r) {
+        hid[r] = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = kb + 32 * (i >> 3) + 8 * g4 + (i & 7);
+          const bool vis = key < see_hi[r] && key >= see_lo[r] && key < k_hi;
+          w[r][i] = vis ? (gp[i >> 3] == -2 ? NAN : w[r][i]) : -INFINITY;
+          hid[r] |= vis ? 0u : 1u << i;
+        }
+      }
+    }
+    if constexpr (ES == 1) scales(scl[b][1], kv);
+#pragma unroll
+    for (int r = 0; r < RS; ++r) {
+      float bmax = w[r][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) bmax = fmaxf(bmax, w[r][i]);
+      bmax *= sc;
+      // The reference moves as in paged_stream; until then no lane needs the
+      // others' maximum.
+      if (__any(bmax > mrun[r] + 8.0f)) {
+        bmax = groups_max(bmax);
+        const bool move = bmax > mrun[r] + 8.0f;
+        const float mnew = move ? bmax : mrun[r];
+        const float corr = move ? __builtin_amdgcn_exp2f(mrun[r] - mnew) : 1.0f;
+        lrun[r] *= corr;
+        mrun[r] = mnew;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[r][d] *= corr;
+      }
+      const float mref = mrun[r] == -INFINITY ? 0.0f : mrun[r];
+      float psum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        w[r][i] = __builtin_amdgcn_exp2f(fmaf(w[r][i], sc, -mref));
+        psum += w[r][i];
+      }
+      lrun[r] += psum;   // this lane's keys
+      if constexpr (ES == 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[r][i] *= kv[i];
+        if (part) {   // a hidden key's scale may be NaN
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[r][i] = hid[r] >> i & 1 ? 0.0f : w[r][i];
+        }
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        pb[r][kk] = make_uint4(pack_bf16x2(w[r][8 * kk], w[r][8 * kk + 1]), pack_bf16x2(w[r][8 * kk + 2], w[r][8 * kk + 3]),
+                               pack_bf16x2(w[r][8 * kk + 4], w[r][8 * kk + 5]), pack_bf16x2(w[r][8 * kk + 6], w[r][8 * kk + 7]));
+    }
+    typedef short v4s_t __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s_t lds_v4s;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const unsigned char* ap = vl + vb[d & 3] + 128 * (d >> 2) + kk * 32 * HD * 2;
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(ap)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(ap + 4 * HD * 2)));
+#pragma unroll
+        for (int r = 0; r < RS; ++r) mma16(o[r][d], make_uint4(lo.x, lo.y, hi.x, hi.y), pb[r][kk], bf16_t());
+      }
+  };
+
+  if (tid == 0) rare = 0;
+  int pg0 = pages(k_lo), pg1 = pages(k_lo + TKB);   // of the block in LDS, of the next one
+  load(k_lo, pg0);
+  __syncthreads();
+  stage(k_lo, 0, pg0);
+  for (int kb = k_lo, b = 0; kb < k_hi; kb += TKB, b ^= 1) {
+    const bool more = kb + TKB < k_hi;
+    if (more) load(kb + TKB, pg1);
+    const int pg2 = pages(kb + 2 * TKB);
+    __syncthreads();          // buffer b is staged, and b ^ 1 no longer read
+    block(kb, b, pg0);
+    if (more) stage(kb + TKB, b ^ 1, pg1);
+    pg0 = pg1;
+    pg1 = pg2;
+  }
+
+  if constexpr (TYPE != VLA_KV_I8) {
+    __syncthreads();
+    if (rare) {
+      for (int kb = k_lo; kb < k_hi; kb += TKB)
+        if (!(kb >= tile_lo && kb + TKB <= min(tile_hi, k_hi))) {
+#pragma unroll
+          for (int s = 0; s < RS; ++s)
+            add_not_finite<TYPE, HD>(p, table, g, kb, min(kb + TKB, k_hi), see_lo[s], see_hi[s], o[s],
+                                     [&](int d, int i) { return 16 * d + 4 * g4 + i; });
+        }
+    }
+  }
+
+  float lsum[RS];
+#pragma unroll
+  for (int s = 0; s < RS; ++s) lsum[s] = groups_sum(lrun[s]);
+  // lane holds O^T[dim 16 d + 4 g4 + i][row r16] of each subtile
+  const bool whole = a.nsplit == 1;
+#pragma unroll
+  for (int s = 0; s < RS; ++s) {
+    const int rr = wrow + 16 * s + r16;
+    if (rr >= t.n * a.R) continue;
+    const int tok = by_r(a, rr), h = g * a.R + mod_r(a, rr);
+    const size_t th = (size_t)(t.s0 + tok) * a.H + h;
+    const float tot = t.beyond ? NAN : lsum[s];
+    if (g4 == 0) {
+      if (!whole) *reinterpret_cast<float2*>(a.stats + ((size_t)split * p.T * a.H + th) * 2) = make_float2(mrun[s], tot);
+      else if (a.lse) a.lse[th] = (mrun[s] + __log2f(tot)) * kLn2;
+    }
+    const float inv = whole ? (tot == 0.0f ? 0.0f : 1.0f / tot) : 1.0f;
+    float* pd = a.part + ((size_t)split * p.T * a.H + th) * HD + 4 * g4;
+    bf16_t* od = reinterpret_cast<bf16_t*>(a.o) + (size_t)(t.s0 + tok) * a.ldo + (size_t)h * HD + 4 * g4;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const float x[4] = {o[s][d][0] * inv, o[s][d][1] * inv, o[s][d][2] * inv, o[s][d][3] * inv};
+      if (!whole) put<float, 4>(pd + 16 * d, x);
+      else put<bf16_t, 4>(od + 16 * d, x);
+    }
   }
 }
 
@@ -565,6 +974,23 @@ hipError_t stream_launch(const PagedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int TYPE, int HD, int RS, int NW, int OCC>
+hipError_t tile_launch(const PagedAttnArgs& a, hipStream_t s) {
+  const long long units = (long long)a.slots * a.p.G * a.nsplit;
+  hipLaunchKernelGGL((paged_tile<TYPE, HD, RS, NW, OCC>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(64 * NW), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t tile_hd(const PagedAttnArgs& a, hipStream_t s) {
+  switch (a.p.hd) {
+    case 64: return tile_launch<TYPE, 64, 2, 4, 2>(a, s);
+    case 128: return tile_launch<TYPE, 128, 2, 4, 2>(a, s);
+    case 256: return tile_launch<TYPE, 256, 1, 8, 2>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
 template <int TYPE>
 hipError_t stream_hd(const PagedAttnArgs& a, hipStream_t s) {
   switch (a.p.hd) {
@@ -579,14 +1005,42 @@ hipError_t stream_hd(const PagedAttnArgs& a, hipStream_t s) {
 
 void paged_attention_plan(PagedAttnArgs& a, long long span) {
   a.rdiv = ((1ull << 32) + a.R - 1) / a.R;
-  a.slots = (int)((long long)a.p.T * a.R / 16) + a.p.B;
-  const long long base = std::max(1LL, (long long)a.slots * a.p.G);
-  // Key splits: about 1536 workgroups (64 requests of up to 8192 rows of int8:
-  // 118 us with 512, 103 with 1536, 116 with 4096), a wave's 32 keys at least:
-  // a CU takes in some 50 GB/s, so a short request is spread wide as well.  Up
-  // to 256 rows one workgroup is done before a second launch would be (72 rows
-  // of fp32: 7.0 us, 9.6 in three splits).
-  a.nsplit = span <= 256 ? 1 : (int)std::max(1LL, std::min({(1536 + base - 1) / base, (span + 31) / 32, 64LL}));
+  const long long rows = (long long)a.p.T * a.R, B = std::max(1, a.p.B), G = a.p.G;
+  // The 128-row tile reads a key once for all rows, but a request with few rows
+  // leaves most of its waves without work: from 32 rows per request where the
+  // tiles are a round of the chip at most (8 requests, 38 rows over 2000 keys:
+  // 22.6 us against 24.0), else from 96 (64 requests over 4000 keys of 128: 66
+  // rows 165 us against 139, 104 rows 185 against 192).  bf16 rows of 256 take a
+  // stream wave's registers twice over; the tile is faster at any number (16 x 1
+  // token of 8 heads over 16000 keys: 57 us against 87).
+  const long long tiles = (rows / 128 + B) * G, fit = a.p.hd == 256 ? 256 : 512;
+  const bool tile = a.p.type != VLA_KV_F32 && ((a.p.type == VLA_KV_BF16 && a.p.hd == 256) || rows >= (2 * tiles <= fit ? 32 : 96) * B);
+  a.rows = tile ? 128 : 16;
+  a.slots = (int)(rows / a.rows) + a.p.B;
+  const long long base = std::max(1LL, a.slots * G);
+  long long n;
+  if (!tile) {
+    // About 1536 workgroups of 96 keys or more (64 requests of up to 8192 rows
+    // of int8: 125 us whole, 95 in 4 splits, 124 in 32), or a workgroup per
+    // compute unit with a wave's 32 keys at least: a CU takes in some 50 GB/s,
+    // so a short request is spread wide as well.  Up to 256 rows one workgroup
+    // is done before a second launch would be (72 rows of fp32: 7.0 us, 9.6 in
+    // three splits).
+    n = span <= 256 ? 1 : std::max(std::min((1536 + base - 1) / base, (span + 95) / 96), std::min(256 / base, (span + 31) / 32));
+  } else if (2 * base <= fit) {
+    // One round of the workgroups that fit the chip (8 x 50 tokens of 8 heads
+    // over 866 rows of 256: 36 us whole, 23 in 5 to 7 splits, 31 in 8, which are
+    // two rounds).
+    n = std::min(fit / base, (span + 63) / 64);
+  } else {
+    // Four rounds, so that long and short requests even out (three prompts of up
+    // to 10007 rows, 715 tiles: 643 us whole, 563 in three splits), as long as
+    // the splits' outputs, written and read in fp32 (about 5 TB/s), take no more
+    // than 15% of the time of the blocks (about 2 us for 64 keys).
+    const double work = (double)base * (span / 64.0) * 2e-6 / fit, outputs = (double)rows * G * a.p.hd * 8 / 5e12;
+    n = std::min((4 * fit + base - 1) / base, (long long)(0.15 * work / std::max(outputs, 1e-12)));
+  }
+  a.nsplit = (int)std::max(1LL, std::min(n, 64LL));
   a.chunk = (int)((span + a.nsplit - 1) / a.nsplit + 31) & ~31;
   if (a.chunk < 32) a.chunk = 32;
 }
@@ -601,9 +1055,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
   switch (a.p.type) {
     case VLA_KV_F32: e = stream_hd<VLA_KV_F32>(a, s); break;
-    case VLA_KV_BF16: e = stream_hd<VLA_KV_BF16>(a, s); break;
-    case VLA_KV_I8: e = stream_hd<VLA_KV_I8>(a, s); break;
-    case VLA_KV_E4M3: e = stream_hd<VLA_KV_E4M3>(a, s); break;
+    case VLA_KV_BF16: e = a.rows == 16 ? stream_hd<VLA_KV_BF16>(a, s) : tile_hd<VLA_KV_BF16>(a, s); break;
+    case VLA_KV_I8: e = a.rows == 16 ? stream_hd<VLA_KV_I8>(a, s) : tile_hd<VLA_KV_I8>(a, s); break;
+    case VLA_KV_E4M3: e = a.rows == 16 ? stream_hd<VLA_KV_E4M3>(a, s) : tile_hd<VLA_KV_E4M3>(a, s); break;
   }
   if (e != hipSuccess || a.nsplit == 1) return e;
   const long long rows = (long long)a.p.T * a.H;

@@ -294,6 +294,7 @@ struct PagedAttnArgs {
   long long ldo;
   float* lse;
   float scale;
+  int rows;                // rows (token, head) of a tile: 16 or 128
   int slots;               // row tiles of all requests, at most (see paged_tile_of)
   int nsplit;              // key splits
   int chunk;               // keys per split (the last one takes the rest)
