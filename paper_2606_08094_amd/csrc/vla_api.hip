@@ -1768,7 +1768,7 @@ vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batc
   PageRowsArgs a{};
   VLA_TRY(serve_sizes(pages, batch, &a.p));
   if (rows < 0) return fail(VLA_E_SHAPE, "negative dimension");
-  if ((long long)a.p.B * a.p.G * (a.p.hd / 16) * rows > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many rows for one call");
+  if ((long long)a.p.B * a.p.G * 2 * ((rows + 31LL) / 32) * 256 > kMaxThreads) return fail(VLA_E_UNSUPPORTED, "too many rows for one call");
   if (rows == 0 || a.p.B == 0) return VLA_OK;
   VLA_TRY(serve_buffers(a.p, false));
   if (!k_out || !v_out || !al16(k_out) || !al16(v_out)) return fail(VLA_E_ARG, "k_out and v_out must be non-NULL and 16-byte aligned");
