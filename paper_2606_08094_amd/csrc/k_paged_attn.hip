@@ -560,9 +560,12 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
 // NW waves takes 16 RS NW rows, RS subtiles of 16 per wave, and walks its keys
 // in blocks of 64 that are staged in LDS as bf16 (8-bit codes are widened once
 // for all rows) and serve every row:
-//   K [64 keys][HD]  16-byte chunk c of key k at slot c ^ kswz(k)
-//   V [64 keys][HD]  16-byte chunk c of key k at slot c ^ vswz(k)
-// kswz gives the eight keys of one bank cycle of a score operand eight slots.
+//   K [64 keys][HD]  16-byte chunk c of key k at slot kslot(c, k)
+//   V [64 keys][HD]  16-byte chunk c of key k at slot vslot(c, k)
+// The slots keep apart modulo 16 (the 64 banks of LDS) the sixteen keys of a
+// score operand (8 i + j, i, j < 4, one chunk), the sixteen pieces of a
+// transposing read (keys 8 i + j, i < 2, j < 4, two chunks), and what sixteen
+// lanes write: chunks of bf16 rows, or the even (odd) chunks of 8-bit rows.
 // V^T operands come from ds_read_b64_tr_b16: within 16 lanes, lane i receives
 // element i % 4 of the 8-byte blocks addressed by lanes i / 4, i / 4 + 4, + 8
 // and + 12, so lane p of group g addresses key 8 g + p / 4 (+ 4 for the second
@@ -571,11 +574,16 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
 // An operand from LDS feeds RS MFMAs.  The next block's rows are on their way
 // in registers, and the page ids of the one after that, while a block is
 // worked on; LDS is double-buffered, one barrier per block.
-VLA_DEV uint4 pick(bool c, const uint4& x, const uint4& y) {   // (by dwords: a select of structs goes through memory)
-  return make_uint4(c ? x.x : y.x, c ? x.y : y.y, c ? x.z : y.z, c ? x.w : y.w);
+template <int HD>
+VLA_DEV int kslot(int c, int k) {
+  if constexpr (HD == 64) return c ^ ((k >> 1 & 1) | (k >> 2 & 6));   // (two rows to 256 bytes)
+  return c ^ (c >> 4) ^ ((k & 3) | (k >> 1 & 12));
 }
-VLA_DEV int kswz(int k) { return (k & 3) | ((k >> 1) & 4); }
-VLA_DEV int vswz(int k) { return 2 * (k & 3); }
+template <int HD>
+VLA_DEV int vslot(int c, int k) {
+  if constexpr (HD == 64) return c ^ ((k >> 1 & 1) * 3 | (k >> 1 & 4));
+  return c ^ (c >> 4) ^ ((k & 1) | (k & 3) << 1 | (k & 8));
+}
 
 constexpr int TKB = 64;   // keys per block
 
@@ -596,14 +604,14 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
   using S = TileShape<TYPE, HD, RS, NW>;
   constexpr int LD = S::LD, CPR = S::CPR, NQV = HD / 32, DT = HD / 16, ES = S::ES;
   __shared__ uint4 st[2][S::BUF];
-  __shared__ __align__(16) float scl[2][2][TKB];   // 8-bit types: scales of the block's keys, K and V
+  __shared__ __align__(16) float scl[2][2][TKB];   // 8-bit types: scales of the block's keys, K (times sc) and V
   __shared__ int rare;                         // V values that are not finite were taken out of a product
 
   const PageArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   const int units = a.slots * p.G * a.nsplit;
-  int u = (int)(blockIdx.x % 8u) * (int)(gridDim.x / 8u) + (int)(blockIdx.x / 8u);
+  int u = a.by_xcd ? (int)(blockIdx.x % 8u) * (int)(gridDim.x / 8u) + (int)(blockIdx.x / 8u) : (int)blockIdx.x;
   if (u >= units) return;
   const int slot = u % a.slots;
   u /= a.slots;
@@ -617,7 +625,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
   const int* table = p.table + (size_t)t.b * p.max_pages;
   const size_t pagerows = (size_t)1 << p.lg;
   const int mask = (1 << p.lg) - 1;
-  const float sc = score_factor(a);
+  const float sc = a.scale * kLog2e;
   // rows of the tile that see every key in [all_lo, all_hi): of tokens i0 .. i1
   auto all_of = [&](int row, int rows, int& lo, int& hi) {
     const int i0 = by_r(a, row), i1 = min(t.n - 1, by_r(a, row + rows - 1));
@@ -658,7 +666,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
       if (wave < 2) {          // lane: key kb + lane, of page group lane / 16
         const size_t row = ((size_t)max(pg, 0) * p.G + g) * pagerows + ((kb + lane) & mask);
         sreg = (wave == 0 ? p.ks : p.vs)[row];
-        if (wave == 0) sreg = pg == -2 ? NAN : sreg;
+        if (wave == 0) sreg = pg == -2 ? NAN : sreg * sc;
         else if (pg < 0) sreg = 0.0f;
       }
     }
@@ -686,19 +694,13 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
       uint4* kl = st[b] + k * CPR;
       uint4* vl = st[b] + (TKB + k) * CPR;
       if constexpr (ES == 1) {
-        // Two chunks each; lanes 4 .. 7 of eight begin with the second, so that
-        // the eight write eight different slots (of K rows of 64 the two keys
-        // in them differ in their swizzle's lowest bit already).
-        const int swv = lane >> 2 & 1, swk = HD == 64 ? 0 : swv;
-        const uint4 k0 = codes_bf16<TYPE>(kr[i].x, kr[i].y), k1 = codes_bf16<TYPE>(kr[i].z, kr[i].w);
-        const uint4 v0 = codes_bf16<TYPE>(v.x, v.y), v1 = codes_bf16<TYPE>(v.z, v.w);
-        kl[(2 * lvec + swk) ^ kswz(k)] = pick(swk, k1, k0);
-        kl[(2 * lvec + 1 - swk) ^ kswz(k)] = pick(swk, k0, k1);
-        vl[(2 * lvec + swv) ^ vswz(k)] = pick(swv, v1, v0);
-        vl[(2 * lvec + 1 - swv) ^ vswz(k)] = pick(swv, v0, v1);
+        kl[kslot<HD>(2 * lvec, k)] = codes_bf16<TYPE>(kr[i].x, kr[i].y);
+        kl[kslot<HD>(2 * lvec + 1, k)] = codes_bf16<TYPE>(kr[i].z, kr[i].w);
+        vl[vslot<HD>(2 * lvec, k)] = codes_bf16<TYPE>(v.x, v.y);
+        vl[vslot<HD>(2 * lvec + 1, k)] = codes_bf16<TYPE>(v.z, v.w);
       } else {
-        kl[lvec ^ kswz(k)] = kr[i];
-        vl[lvec ^ vswz(k)] = v;
+        kl[kslot<HD>(lvec, k)] = kr[i];
+        vl[vslot<HD>(lvec, k)] = v;
       }
     }
     if constexpr (ES == 1) {
@@ -730,20 +732,27 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
 #pragma unroll
     for (int c = 0; c < NQV; ++c) qf[s][c] = rok ? ldg16(qp + 8 * c) : make_uint4(0, 0, 0, 0);
   }
-  // LDS operand places of this lane: score row r16 is key 32 kk + 4 tt + 8 (r16 / 4) + r16 % 4
-  const int kkey = 8 * (r16 >> 2) + (r16 & 3), kf = kswz(kkey);
-  int vb[4];   // byte offset of the V^T reads of dim tiles d with d % 4 == q; tile d adds 128 (d / 4)
-  {
-    const int q4 = r16 >> 2, rowb = (8 * g4 + q4) * HD * 2;
+  // LDS operand places of this lane: score row r16 is key 32 kk + 4 tt + 8 (r16
+  // / 4) + r16 % 4 (the slots of a chunk do not depend on kk and tt), and chunk
+  // g4 NQV + c of it.
+  const int kkey = 8 * (r16 >> 2) + (r16 & 3);
+  int kat[NQV];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) vb[q] = rowb + (((2 * q + ((r16 & 3) >> 1)) ^ (2 * q4)) * 16) + (r16 & 1) * 8;
+  for (int c = 0; c < NQV; ++c) kat[c] = kkey * CPR + kslot<HD>(g4 * NQV + c, kkey);
+  // V^T reads of dim tile d: key 8 g4 + r16 / 4 (+ 4, + 32: the same slots), chunk 2 d + (r16 % 4) / 2
+  int vat[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    const int k = 8 * g4 + (r16 >> 2);
+    vat[d] = k * HD * 2 + vslot<HD>(2 * d + ((r16 & 3) >> 1), k) * 16 + (r16 & 1) * 8;
   }
 
   f32x4 o[RS][DT];
-  float mrun[RS], lrun[RS];
+  float mref[RS], limit[RS], lrun[RS];   // reference of the exponentials; how far above it a score may be
 #pragma unroll
   for (int s = 0; s < RS; ++s) {
-    mrun[s] = -INFINITY;
+    mref[s] = 0.0f;
+    limit[s] = -INFINITY;
     lrun[s] = 0.0f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[s][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -774,7 +783,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-          const uint4 kv = kl[(kkey + 32 * kk + 4 * tt) * CPR + ((g4 * NQV + c) ^ kf)];
+          const uint4 kv = kl[kat[c] + (32 * kk + 4 * tt) * CPR];
 #pragma unroll
           for (int r = 0; r < RS; ++r) mma16(s[r][kk][tt], kv, qf[r][c], bf16_t());
         }
@@ -783,13 +792,12 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
     uint4 pb[RS][2];
     float w[RS][16], kv[16];
     unsigned hid[RS];
+    // scores less the reference (base 2): one operation each
     if constexpr (ES == 1) scales(scl[b][0], kv);
 #pragma unroll
     for (int r = 0; r < RS; ++r)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[r][i] = ES == 1 ? s[r][i >> 3][i >> 2 & 1][i & 3] * kv[i] : s[r][i >> 3][i >> 2 & 1][i & 3];
-#pragma unroll
-    for (int r = 0; r < RS; ++r) turn_scores(a, w[r]);
+      for (int i = 0; i < 16; ++i) w[r][i] = fmaf(s[r][i >> 3][i >> 2 & 1][i & 3], ES == 1 ? kv[i] : sc, -mref[r]);
     if (part) {
       int gp[2];      // pages of this lane's keys
 #pragma unroll
@@ -812,24 +820,26 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
       float bmax = w[r][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) bmax = fmaxf(bmax, w[r][i]);
-      bmax *= sc;
-      // The reference moves as in paged_stream; until then no lane needs the
-      // others' maximum.
-      if (__any(bmax > mrun[r] + 8.0f)) {
+      // The reference moves as in paged_stream, and from the first visible key on
+      // (limit is 8, before that -infinity); until then no lane needs the others'
+      // maximum.
+      if (__any(bmax > limit[r])) {
         bmax = groups_max(bmax);
-        const bool move = bmax > mrun[r] + 8.0f;
-        const float mnew = move ? bmax : mrun[r];
-        const float corr = move ? __builtin_amdgcn_exp2f(mrun[r] - mnew) : 1.0f;
-        lrun[r] *= corr;
-        mrun[r] = mnew;
+        if (bmax > limit[r]) {
+          const float corr = limit[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-bmax);
+          limit[r] = 8.0f;
+          mref[r] += bmax;
+          lrun[r] *= corr;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[r][d] *= corr;
+          for (int d = 0; d < DT; ++d) o[r][d] *= corr;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[r][i] -= bmax;
+        }
       }
-      const float mref = mrun[r] == -INFINITY ? 0.0f : mrun[r];
       float psum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        w[r][i] = __builtin_amdgcn_exp2f(fmaf(w[r][i], sc, -mref));
+        w[r][i] = __builtin_amdgcn_exp2f(w[r][i]);
         psum += w[r][i];
       }
       lrun[r] += psum;   // this lane's keys
@@ -852,7 +862,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        const unsigned char* ap = vl + vb[d & 3] + 128 * (d >> 2) + kk * 32 * HD * 2;
+        const unsigned char* ap = vl + vat[d] + kk * 32 * HD * 2;
         const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(ap)));
         const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(ap + 4 * HD * 2)));
 #pragma unroll
@@ -889,9 +899,12 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
     }
   }
 
-  float lsum[RS];
+  float lsum[RS], mrun[RS];
 #pragma unroll
-  for (int s = 0; s < RS; ++s) lsum[s] = groups_sum(lrun[s]);
+  for (int s = 0; s < RS; ++s) {
+    lsum[s] = groups_sum(lrun[s]);
+    mrun[s] = limit[s] == -INFINITY ? -INFINITY : mref[s];
+  }
   // lane holds O^T[dim 16 d + 4 g4 + i][row r16] of each subtile
   const bool whole = a.nsplit == 1;
 #pragma unroll
@@ -1041,6 +1054,11 @@ void paged_attention_plan(PagedAttnArgs& a, long long span) {
     n = std::min((4 * fit + base - 1) / base, (long long)(0.15 * work / std::max(outputs, 1e-12)));
   }
   a.nsplit = (int)std::max(1LL, std::min(n, 64LL));
+  // Consecutive tiles on one XCD read the same keys through its L2; in many
+  // rounds tiles of unequal length had better go to all XCDs in turn (4 x 600
+  // tokens over 4000 keys, one round: 95 us against 102; three prompts of up to
+  // 10007 rows: 560 us against 545).
+  a.by_xcd = base * a.nsplit <= 2 * fit;
   a.chunk = (int)((span + a.nsplit - 1) / a.nsplit + 31) & ~31;
   if (a.chunk < 32) a.chunk = 32;
 }

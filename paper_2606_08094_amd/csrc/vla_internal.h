@@ -296,8 +296,9 @@ struct PagedAttnArgs {
   float scale;
   int rows;                // rows (token, head) of a tile: 16 or 128
   int slots;               // row tiles of all requests, at most (see paged_tile_of)
-  int nsplit;              // key splits
-  int chunk;               // keys per split (the last one takes the rest)
+  int nsplit;              // key splits, at most, of one request
+  int chunk;               // keys for which a request takes one more split
+  int by_xcd;              // tile kernel: consecutive tiles on one XCD, else in turn over all
   float* part;             // [nsplit][T][H][hd]: unnormalised output of each split (nsplit > 1)
   float* stats;            // [nsplit][T][H][2]: its (max, sum)
 };

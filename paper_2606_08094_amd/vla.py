@@ -326,37 +326,61 @@ def ternary_gemm(x, w_packed, M: int, N: int, K: int, acc_out, stream=None):
 
 # ---- 8-bit serving operators -------------------------------------------------
 
-def _raw_stream(index: int) -> int:
-    """Handle of a device's current stream (through the call that makes no
-    Stream object, where this torch has it: 0.1 us instead of 2.7)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
+_now = None   # (current device, current stream of a device): set by the first call
 
 
-def _launch(f, where, stream, *args):
-    """f(*args, stream handle), with the device of tensor `where` as the current
-    one; a stream of None is that device's current stream."""
+def _bind_torch():
+    """The calls that make no Stream object, where this torch has them (0.1 us
+    instead of 2.9 for device and stream)."""
+    global _now
     import torch
-    now = torch.cuda.current_device()
-    index = getattr(getattr(where, "device", None), "index", None)
-    if index is None or index == now:
-        return _check(f(*args, _raw_stream(now) if stream is None else _stream(stream)))
-    with torch.cuda.device(index):
-        return _check(f(*args, _raw_stream(index) if stream is None else _stream(stream)))
+    torch.cuda.init()
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _now = (device, stream)
+    return _now
+
+
+def _launch(f, index: int, stream, *args):
+    """f(*args, stream handle) with device `index` (-1: whichever is current) as
+    the current one; a stream of None is that device's current stream."""
+    device, current = _now or _bind_torch()
+    now = device()
+    if index < 0 or index == now:
+        st = f(*args, current(now) if stream is None else _stream(stream))
+    else:
+        import torch
+        with torch.cuda.device(index):
+            st = f(*args, current(index) if stream is None else _stream(stream))
+    if st:
+        _check(st)
+
+
+def _device(x) -> int:
+    """Index of a tensor's device, -1 for a raw address."""
+    return -1 if x is None or isinstance(x, int) else x.get_device()
+
+
+def _gpu(x) -> Optional[int]:
+    """Address of a tensor in device memory, of which a host tensor is none."""
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_cuda:
+        raise VlaError(1, "a tensor is not in device memory")
+    return x.data_ptr()
 
 
 def quantize_tokens(elem: int, x, M: int, K: int, ldx: int, q, ldq: int, r, stream=None):
     """Per-token int8 codes q [M][ldq] and absolute maxima r [M] of x [M][ldx]
     (elem: 0 fp32, 1 bf16)."""
-    _launch(lib().vla_quantize_tokens, x, stream, elem, _ptr(x), M, K, ldx, _ptr(q), ldq, _ptr(r))
+    _launch(lib().vla_quantize_tokens, _device(x), stream, elem, _gpu(x), M, K, ldx, _gpu(q), ldq, _gpu(r))
 
 
 def int8_gemm(q, ldq: int, r, w, ldw: int, w_scale, bias, M: int, N: int, K: int, elem: int, y, ldy: int, stream=None):
     """y [M][ldy] = (q w^T) * (w_scale[n] * r[m] / 127) + bias: int8 codes q, r of
     quantize_tokens, int8 weights w [N][ldw] with a scale per channel."""
-    _launch(lib().vla_int8_gemm, q, stream, _ptr(q), ldq, _ptr(r), _ptr(w), ldw, _ptr(w_scale), _ptr(bias), M, N, K, elem,
-            _ptr(y), ldy)
+    _launch(lib().vla_int8_gemm, _device(q), stream, _gpu(q), ldq, _gpu(r), _gpu(w), ldw, _gpu(w_scale), _gpu(bias), M, N, K, elem,
+            _gpu(y), ldy)
 
 
 class KVPages:
@@ -367,8 +391,10 @@ class KVPages:
     def __init__(self, type: str, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k, v, k_scale=None,
                  v_scale=None):
         self.tensors = (k, v, k_scale, v_scale)   # the struct holds addresses only
-        self._c = VlaKvPages(KV_TYPES[type], n_pages, page_size, n_kv_heads, head_dim, _ptr(k), _ptr(v), _ptr(k_scale),
-                             _ptr(v_scale))
+        self._c = VlaKvPages(KV_TYPES[type], n_pages, page_size, n_kv_heads, head_dim, _gpu(k), _gpu(v), _gpu(k_scale),
+                             _gpu(v_scale))
+        self._ref = ctypes.byref(self._c)
+        self.device = _device(k)
 
 
 class KVBatch:
@@ -377,22 +403,23 @@ class KVBatch:
 
     def __init__(self, n_requests: int, max_pages: int, n_tokens: int, max_len: int, page_table, kv_len, q_start=None):
         self.tensors = (page_table, kv_len, q_start)
-        self._c = VlaKvBatch(n_requests, max_pages, n_tokens, max_len, _ptr(page_table), _ptr(kv_len), _ptr(q_start))
+        self._c = VlaKvBatch(n_requests, max_pages, n_tokens, max_len, _gpu(page_table), _gpu(kv_len), _gpu(q_start))
+        self._ref = ctypes.byref(self._c)
 
 
 def kv_pages_write(pages: KVPages, batch: KVBatch, elem: int, k, v, token_stride: int, head_stride: int, stream=None):
     """The new tokens' keys and values into their pages, quantised as the pages are."""
-    _launch(lib().vla_kv_pages_write, pages.tensors[0], stream, pages._c, batch._c, elem, _ptr(k), _ptr(v), token_stride,
+    _launch(lib().vla_kv_pages_write, pages.device, stream, pages._ref, batch._ref, elem, _gpu(k), _gpu(v), token_stride,
             head_stride)
 
 
 def kv_pages_read(pages: KVPages, batch: KVBatch, rows: int, elem: int, k_out, v_out, stream=None):
     """The first `rows` rows of every request as k_out, v_out [n_requests][n_kv_heads][rows][head_dim]."""
-    _launch(lib().vla_kv_pages_read, pages.tensors[0], stream, pages._c, batch._c, rows, elem, _ptr(k_out), _ptr(v_out))
+    _launch(lib().vla_kv_pages_read, pages.device, stream, pages._ref, batch._ref, rows, elem, _gpu(k_out), _gpu(v_out))
 
 
 def paged_attention_workspace(pages: KVPages, batch: KVBatch, n_heads: int) -> int:
-    n = lib().vla_paged_attention_workspace(pages._c, batch._c, n_heads)
+    n = lib().vla_paged_attention_workspace(pages._ref, batch._ref, n_heads)
     if n == ctypes.c_size_t(-1).value:
         raise VlaError(2, lib().vla_last_error().decode())
     return n
@@ -402,8 +429,8 @@ def paged_attention(pages: KVPages, batch: KVBatch, n_heads: int, elem: int, q, 
                     causal: bool = False, window: int = 0, lse=None, workspace=None, workspace_bytes: int = 0,
                     stream=None):
     """Attention of the new tokens q [n_tokens][ldq] over the pages of their requests."""
-    _launch(lib().vla_paged_attention, pages.tensors[0], stream, pages._c, batch._c, n_heads, elem, _ptr(q), ldq, _ptr(o),
-            ldo, float(scale), int(bool(causal)), int(window), _ptr(lse), _ptr(workspace), workspace_bytes)
+    _launch(lib().vla_paged_attention, pages.device, stream, pages._ref, batch._ref, n_heads, elem, _gpu(q), ldq, _gpu(o),
+            ldo, float(scale), int(bool(causal)), int(window), _gpu(lse), _gpu(workspace), workspace_bytes)
 
 
 # ---- test-only per-kernel entries (include/vla_test.h) ---------------------

@@ -178,3 +178,26 @@ def test_workspace_covers_every_window(vla):
         for window in (0, 1, 31, 1000, 50000, 2 ** 31 - 1):
             got = L.vla_paged_attention(p, b, 4, 1, None, 512, 16, 512, 0.1, 1, window, None, 16, need, None)
             assert status(vla, got) == "VLA_E_ARG" and b"q and o" in L.vla_last_error()
+
+
+def test_binding_turns_host_tensors_away(vla):
+    """A host tensor's address would be read by a kernel: refused before the call."""
+    import torch
+    x = torch.zeros(2, 64)
+    with pytest.raises(vla.VlaError, match="device memory"):
+        vla.KVPages("f32", 1, 16, 1, 64, x, x)
+    with pytest.raises(vla.VlaError, match="device memory"):
+        vla.KVBatch(1, 1, 1, 1, x, 16, 16)
+    for f, args in ((vla.quantize_tokens, (0, x, 2, 64, 64, 16, 64, 16)),
+                    (vla.int8_gemm, (16, 64, 16, 16, 64, 16, x, 2, 2, 64, 0, 16, 2))):
+        with pytest.raises(vla.VlaError, match="device memory"):
+            f(*args)
+
+
+def test_binding_reports_what_the_library_refuses(vla):
+    p = vla.KVPages("i8", 4, 48, 2, 128, 16, 16, 16, 16)
+    b = vla.KVBatch(2, 2, 3, 60, 16, 16, 16)
+    with pytest.raises(vla.VlaError, match="power of two"):
+        vla.paged_attention_workspace(p, b, 2)
+    with pytest.raises(KeyError):
+        vla.KVPages("fp4", 4, 32, 2, 128, 16, 16)
