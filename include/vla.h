@@ -323,7 +323,7 @@ vla_status vla_prefix_prefill(vla_backbone* backbone, const void* embeds, int32_
  * overlap (other streams, other threads) as long as none writes what another
  * uses, and may be captured into a HIP graph; what lies in device memory
  * (lengths, page tables) is read when the work runs, so a replay sees its
- * present values.  Lengths and page ids in device memory cannot be refused by
+ * present values.  The buffers are on the current device.  Lengths and page ids in device memory cannot be refused by
  * the host: the kernels bound every access by what the call says, and what is
  * said below of ids outside the pool holds.  `elem`, the type of rows that
  * come or go: VLA_T_F32 or VLA_T_BF16.  Pitches and strides count elements.

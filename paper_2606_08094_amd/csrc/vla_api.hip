@@ -1700,7 +1700,7 @@ vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int3
   if (window > 0) span = std::min(span, window + 1024);
   a->window = window;
   paged_attention_plan(*a, span);
-  if ((long long)a->slots * a->p.G * a->nsplit * 256 > kMaxThreads || (long long)a->p.T * a->H * 64 > kMaxThreads)
+  if ((long long)a->slots * a->p.G * a->nsplit * 512 > kMaxThreads || (long long)a->p.T * a->H * 64 > kMaxThreads)
     return fail(VLA_E_UNSUPPORTED, "too many tokens and heads for one call");
   return VLA_OK;
 }

@@ -304,7 +304,7 @@ def test_read_marks_rows_without_a_page(torch, vla):
 # ---- paged attention ---------------------------------------------------------------
 
 def check_attention(torch, vla, P, R, causal, window, max_len=None, starts=None, lens=None, ldq_extra=0, in_place=False,
-                    with_lse=True, scale=None, stream=None):
+                    with_lse=True, scale=None, heads=None):
     """Run paged_attention on P's filled pool and compare every new token with the definition."""
     G, hd = P.G, P.hd
     H = G * R
@@ -334,7 +334,7 @@ def check_attention(torch, vla, P, R, causal, window, max_len=None, starts=None,
         mine[s0:s1] = True
         pos = L - (s1 - s0) + np.arange(s1 - s0)
         k, v = P.values(b, 0)[:L], P.values(b, 1)[:L]
-        for h in range(H):
+        for h in heads or range(H):
             want, wl_, mag, big = ref.attention(q[s0:s1, h * hd:(h + 1) * hd].astype(np.float64), k[:, h // R], v[:, h // R],
                                                 pos, scale, causal, window)
             # scores: hd products and a few roundings of scale and code scale; a score off by d moves p by d,
@@ -417,6 +417,21 @@ def test_paged_attention_many_requests(torch, vla, kind):
     P = Paged(torch, vla, kind, 64, 1, 16, lens, news, pad=5)
     P.fill()
     check_attention(torch, vla, P, 2, True, 0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "i8", "e4m3"])
+@pytest.mark.parametrize("hd,G,R,lens,news", [
+    (64, 4, 16, [900, 100, 2100], [800, 90, 1300]),        # tiles for several rounds of the chip
+    (128, 8, 1, [3000, 40, 5000, 1], [1, 1, 1, 1]),        # one token each, the keys in many splits
+    (256, 1, 8, [4000, 500], [1, 3]),
+    (128, 1, 4, [9000], [40]),                             # one round of tiles, the keys in many splits
+])
+def test_paged_attention_at_size(torch, vla, kind, hd, G, R, lens, news):
+    """The shapes whose work is spread in other ways; some heads of each."""
+    P = Paged(torch, vla, kind, hd, G, 64, lens, news, seed=11, pad=1)
+    P.fill()
+    check_attention(torch, vla, P, R, True, 0, heads=[0, G * R - 1])
+    check_attention(torch, vla, P, R, True, 700, heads=[G * R // 2])
 
 
 @pytest.mark.parametrize("kind,hd", [("bf16", 128), ("f32", 64), ("i8", 256)])
