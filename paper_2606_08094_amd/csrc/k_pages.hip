@@ -176,9 +176,12 @@ void write_nt(const PageRowsArgs& a, hipStream_t s) {
 }
 template <int F32, int TYPE, int HD>
 hipError_t write_hd(const PageRowsArgs& a, hipStream_t s) {
-  // as many tokens per wave as leave waves for the whole chip
+  // As many tokens per wave as leave some rounds of waves, whose lookups then
+  // overlap with others' rows (16 x 2048 rows of 256 at most, int8: 11.4 us with
+  // 16 tokens, 10.2 with 8; 16 x 4096 x 8 heads of 128: the same).
   const long long rows = (long long)a.p.T * 2 * a.p.G;
-  if (rows >= 16 * 2048) write_nt<F32, TYPE, HD, 16>(a, s);
+  if (rows >= 64 * 2048) write_nt<F32, TYPE, HD, 16>(a, s);
+  else if (rows >= 16 * 2048) write_nt<F32, TYPE, HD, 8>(a, s);
   else if (rows >= 4 * 2048) write_nt<F32, TYPE, HD, 4>(a, s);
   else write_nt<F32, TYPE, HD, 1>(a, s);
   return hipGetLastError();
