@@ -368,7 +368,7 @@ typedef struct vla_kv_pages {
   int32_t n_pages;      /* pages of the pool */
   int32_t page_size;    /* rows (tokens) of a page: a power of two, 16 .. 1024 */
   int32_t n_kv_heads;   /* G */
-  int32_t head_dim;     /* hd: 64, 128 or 256 (VLA_KV_F32: 64 or 128) */
+  int32_t head_dim;     /* hd: 64, 128 or 256 */
   void* k;              /* [n_pages][G][page_size][hd] */
   void* v;
   float* k_scale;       /* [n_pages][G][page_size]; 8-bit types only */
@@ -428,7 +428,8 @@ vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batc
  *   q, o [n_tokens][ldq / ldo] in elem, head h at column h * hd (they may be
  *   the same array); lse [n_tokens][n_heads] fp32 or NULL.  elem is VLA_T_F32
  *   for VLA_KV_F32 pages and VLA_T_BF16 for the others.
- *   n_heads a multiple of G, at most 16 G; ldq, ldo multiples of 16 bytes.
+ *   n_heads a multiple of G, at most 16 G; ldq, ldo multiples of 16 bytes;
+ *   over VLA_KV_F32 pages head_dim is 64 or 128.
  *   workspace: at least vla_paged_attention_workspace bytes (16-byte aligned;
  *   may be NULL if that is 0), used until the work is done: calls that may
  *   overlap, and captured graphs that may, need one each.

@@ -198,11 +198,10 @@ hipError_t read_hd(const PageRowsArgs& a, hipStream_t s) {
 template <typename F>
 hipError_t by_type(int f32, int type, int hd, F f) {
   auto h = [&](auto e, auto t) {
-    constexpr int T = decltype(t)::value;
     switch (hd) {
       case 64: return f(e, t, std::integral_constant<int, 64>{});
       case 128: return f(e, t, std::integral_constant<int, 128>{});
-      case 256: if constexpr (T != VLA_KV_F32) return f(e, t, std::integral_constant<int, 256>{});
+      case 256: return f(e, t, std::integral_constant<int, 256>{});
     }
     return hipErrorInvalidValue;
   };

@@ -1663,8 +1663,8 @@ vla_status serve_sizes(const vla_kv_pages* p, const vla_kv_batch* b, PageArgs* a
     return fail(VLA_E_SHAPE, "negative or zero size in pages or batch");
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
     return fail(VLA_E_SHAPE, "page_size %d is not a power of two in 16..1024", p->page_size);
-  if (!(p->head_dim == 64 || p->head_dim == 128 || (p->head_dim == 256 && p->type != VLA_KV_F32)))
-    return fail(VLA_E_UNSUPPORTED, "head_dim %d unsupported (64, 128%s)", p->head_dim, p->type == VLA_KV_F32 ? "" : ", 256");
+  if (!(p->head_dim == 64 || p->head_dim == 128 || p->head_dim == 256))
+    return fail(VLA_E_UNSUPPORTED, "head_dim %d unsupported (64, 128, 256)", p->head_dim);
   if (p->n_kv_heads > 256) return fail(VLA_E_UNSUPPORTED, "more than 256 K/V heads");
   if (b->n_requests > 65536) return fail(VLA_E_UNSUPPORTED, "more than 65536 requests");
   if (b->n_tokens > (1 << 24)) return fail(VLA_E_UNSUPPORTED, "more than 2^24 new tokens");
@@ -1692,6 +1692,7 @@ vla_status serve_buffers(const PageArgs& a, bool starts) {
 // The attention's arguments that its plan depends on.
 vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, long long window, PagedAttnArgs* a) {
   VLA_TRY(serve_sizes(pages, batch, &a->p));
+  if (a->p.type == VLA_KV_F32 && a->p.hd == 256) return fail(VLA_E_UNSUPPORTED, "attention over fp32 pages: head_dim 64 or 128");
   if (n_heads < 1 || n_heads % a->p.G) return fail(VLA_E_SHAPE, "n_heads %d is not a multiple of %d K/V heads", n_heads, a->p.G);
   a->H = n_heads;
   a->R = n_heads / a->p.G;

@@ -205,8 +205,6 @@ CACHE = [  # hd, G, page, lengths
 def test_write_and_read_back(torch, vla, kind, source, hd, G, page, lens):
     """Codes, scales and values bit for bit; rows and pages of nobody untouched;
     rows behind a request's last untouched in the output."""
-    if kind == "f32" and hd == 256:
-        pytest.skip("fp32 pages have head dimensions 64 and 128")
     P = Paged(torch, vla, kind, hd, G, page, lens, lens, seed=hd + G)
     P.elem = source
     P.rows = [[ref.rounded(P.rng.standard_normal((n, G, hd)).astype(np.float32), source) for _ in range(2)] for n in lens]
@@ -382,7 +380,7 @@ SHAPES = [  # hd, G, R, page, lengths, new tokens
 @pytest.mark.parametrize("hd,G,R,page,lens,news", SHAPES)
 def test_paged_attention(torch, vla, kind, causal, window, hd, G, R, page, lens, news):
     if kind == "f32" and hd == 256:
-        pytest.skip("fp32 pages have head dimensions 64 and 128")
+        pytest.skip("attention over fp32 pages: head dimensions 64 and 128")
     P = Paged(torch, vla, kind, hd, G, page, lens, news, seed=hd + R, pad=2)
     P.fill()
     check_attention(torch, vla, P, R, causal, window)

@@ -62,7 +62,7 @@ BAD_SIZES = [
     (dict(n_pages=0), {}, "VLA_E_SHAPE"), (dict(n_kv_heads=0), {}, "VLA_E_SHAPE"),
     (dict(n_kv_heads=257), {}, "VLA_E_UNSUPPORTED"),
     (dict(page_size=8), {}, "VLA_E_SHAPE"), (dict(page_size=48), {}, "VLA_E_SHAPE"), (dict(page_size=2048), {}, "VLA_E_SHAPE"),
-    (dict(head_dim=96), {}, "VLA_E_UNSUPPORTED"), (dict(type=0, head_dim=256), {}, "VLA_E_UNSUPPORTED"),
+    (dict(head_dim=96), {}, "VLA_E_UNSUPPORTED"), (dict(type=0, head_dim=512), {}, "VLA_E_UNSUPPORTED"),
     ({}, dict(n_requests=-1), "VLA_E_SHAPE"), ({}, dict(n_requests=65537), "VLA_E_UNSUPPORTED"),
     ({}, dict(max_pages=0), "VLA_E_SHAPE"), ({}, dict(max_pages=1 << 26), "VLA_E_SHAPE"),
     ({}, dict(n_tokens=-1), "VLA_E_SHAPE"), ({}, dict(n_tokens=(1 << 24) + 1), "VLA_E_UNSUPPORTED"),
@@ -155,6 +155,13 @@ def test_paged_attention_refusals(vla, change, want):
     got = vla.lib().vla_paged_attention(p, b, a["heads"], a["elem"], a["q"], a["ldq"], a["o"], a["ldo"], a["scale"],
                                         a["causal"], a["window"], a["lse"], 16, 1 << 45, None)
     assert status(vla, got) == want, vla.lib().vla_last_error()
+
+
+def test_attention_over_fp32_pages_of_256_is_refused(vla):
+    p, b = structs(vla, dict(type=0, head_dim=256), {})
+    L = vla.lib()
+    assert L.vla_paged_attention_workspace(p, b, 2) == ctypes.c_size_t(-1).value
+    assert status(vla, L.vla_paged_attention(p, b, 2, 0, 16, 512, 16, 512, 1.0, 0, 0, None, 16, 1 << 40, None)) == "VLA_E_UNSUPPORTED"
 
 
 def test_paged_attention_workspace_is_checked(vla):
