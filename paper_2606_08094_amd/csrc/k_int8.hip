@@ -459,25 +459,12 @@ hipError_t launch_quantize_tokens(int f32, const QuantTokArgs& a, hipStream_t s)
 
 hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
-  if (a.M <= 64) {
-    const bool two = a.N >= 16 * 2 * 256;
-    switch ((a.M <= 16 ? 10 : a.M <= 32 ? 20 : 40) + two) {
-      case 10: skinny_launch<1, 1>(a, s); break;
-      case 11: skinny_launch<1, 2>(a, s); break;
-      case 20: skinny_launch<2, 1>(a, s); break;
-      case 21: skinny_launch<2, 2>(a, s); break;
-      case 40: skinny_launch<4, 1>(a, s); break;
-      default: skinny_launch<4, 2>(a, s); break;
-    }
-    return hipGetLastError();
-  }
-  // Above that, the tile whose rounds over 256 compute units cost least.
-  // Microseconds per 128-deep slice and per round beside the slices (first
-  // loads, output), measured at 8192 x 16384 x 1024 .. 4096: a CU takes in about
-  // 45 GB/s (256 x 256) to 71 GB/s (64 x 128), so large tiles win where they
-  // fill the chip (816 x 16384 x 2048: 33.7 us, 46.4 us on 128 x 128) and small
-  // ones where they would not (816 x 2048 x 16384: 44 us on 64 x 128, 179 us on
-  // 256 x 256).
+  // The tile whose rounds over 256 compute units cost least.  Microseconds per
+  // 128-deep slice and per round beside the slices (first loads, output),
+  // measured at 8192 x 16384 x 1024 .. 4096: a CU takes in about 45 GB/s (256 x
+  // 256) to 71 GB/s (64 x 128), so large tiles win where they fill the chip
+  // (816 x 16384 x 2048: 33.7 us, 46.4 us on 128 x 128) and small ones where
+  // they would not (816 x 2048 x 16384: 44 us on 64 x 128, 179 us on 256 x 256).
   struct Cost { int bm, bn; float slice, round; void (*launch)(Int8Args, hipStream_t); };
   static const Cost costs[] = {{256, 256, 1.50f, 9.8f, tile_launch<16, 8, 1>}, {128, 256, 0.88f, 7.3f, tile_launch<8, 8, 1>},
                                {128, 128, 0.57f, 4.5f, tile_launch<8, 4, 1>},  {64, 128, 0.34f, 3.2f, tile_launch<4, 4, 2>},
@@ -489,6 +476,23 @@ hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s) {
     const float t = (float)((tiles + 255) / 256) * ((float)((a.K + 127) / 128) * c.slice + c.round);
     if (!best || t < least) best = &c, least = t;
   }
-  best->launch(a, s);
+  // Up to 64 tokens the skinny kernel, which spreads K, is ahead where there are
+  // few columns (a workgroup takes in about 36 GB/s of its rows of W and the
+  // tokens'): 36 x 20 x 13120 in 16 us, 1 x 2560 x 2560 in 4.4, but 64 x 16384 x
+  // 8192 in 60 us against 32 on tiles.
+  const bool two = a.N >= 16 * 2 * 256;
+  const float wide = two ? 32.0f : 16.0f, rounds = (float)(((long long)(a.N + (int)wide - 1) / (int)wide + 255) / 256);
+  if (a.M <= 64 && rounds * (wide + (float)a.M) * (float)a.K / 36e3f + 3.0f < least) {
+    switch ((a.M <= 16 ? 10 : a.M <= 32 ? 20 : 40) + two) {
+      case 10: skinny_launch<1, 1>(a, s); break;
+      case 11: skinny_launch<1, 2>(a, s); break;
+      case 20: skinny_launch<2, 1>(a, s); break;
+      case 21: skinny_launch<2, 2>(a, s); break;
+      case 40: skinny_launch<4, 1>(a, s); break;
+      default: skinny_launch<4, 2>(a, s); break;
+    }
+  } else {
+    best->launch(a, s);
+  }
   return hipGetLastError();
 }
