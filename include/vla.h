@@ -323,10 +323,11 @@ vla_status vla_prefix_prefill(vla_backbone* backbone, const void* embeds, int32_
  * overlap (other streams, other threads) as long as none writes what another
  * uses, and may be captured into a HIP graph; what lies in device memory
  * (lengths, page tables) is read when the work runs, so a replay sees its
- * present values.  The buffers are on the current device.  Lengths and page ids in device memory cannot be refused by
- * the host: the kernels bound every access by what the call says, and what is
- * said below of ids outside the pool holds.  `elem`, the type of rows that
- * come or go: VLA_T_F32 or VLA_T_BF16.  Pitches and strides count elements.
+ * present values.  The buffers are on the current device.  Lengths and page ids
+ * in device memory cannot be refused by the host: the kernels bound every
+ * access by what the call says, and what is said below of ids outside the pool
+ * holds.  `elem`, the type of rows that come or go: VLA_T_F32 or VLA_T_BF16.
+ * Pitches and strides count elements.
  * Errors of every call: VLA_E_ARG, VLA_E_SHAPE, VLA_E_UNSUPPORTED, VLA_E_DEVICE. */
 enum { VLA_T_F32 = 0, VLA_T_BF16 = 1 };
 
@@ -380,7 +381,7 @@ typedef struct vla_kv_pages {
  * rows t of one array: those of request b are q_start[b] .. q_start[b+1]-1, and
  * they are its last rows, kv_len[b] - n_b .. kv_len[b]-1, in order (n_b their
  * number).  Rows of that array outside q_start[0] .. q_start[n_requests]-1
- * (padding) are neither read nor written.  A negative kv_len counts as 0. */
+ * (padding) have no influence and are not written.  A negative kv_len counts as 0. */
 typedef struct vla_kv_batch {
   int32_t n_requests;         /* 0 .. 65536 */
   int32_t max_pages;          /* entries of a request's page table; max_pages * page_size <= 2^30 */
@@ -426,10 +427,9 @@ vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batc
  * row of a page outside the pool gets NaN, and so do all tokens of a request
  * whose kv_len is past its page table.
  *   q, o [n_tokens][ldq / ldo] in elem, head h at column h * hd (they may be
- *   the same array); lse [n_tokens][n_heads] fp32 or NULL.  elem is VLA_T_F32
- *   for VLA_KV_F32 pages and VLA_T_BF16 for the others.
- *   n_heads a multiple of G, at most 16 G; ldq, ldo multiples of 16 bytes;
- *   over VLA_KV_F32 pages head_dim is 64 or 128.
+ *   the same array with the same pitch); lse [n_tokens][n_heads] fp32 or NULL.
+ *   elem is VLA_T_F32 for VLA_KV_F32 pages and VLA_T_BF16 for the others.
+ *   n_heads a multiple of G, at most 16 G; ldq, ldo multiples of 16 bytes.
  *   workspace: at least vla_paged_attention_workspace bytes (16-byte aligned;
  *   may be NULL if that is 0), used until the work is done: calls that may
  *   overlap, and captured graphs that may, need one each.

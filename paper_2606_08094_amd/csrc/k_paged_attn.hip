@@ -266,7 +266,7 @@ VLA_DEV void add_not_finite(const PageArgs& p, const int* table, int g, int k0, 
 // they do without spilling.
 template <int TYPE, int HD>
 constexpr int stream_occupancy() {
-  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : 2) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : HD == 128 ? 3 : 1) : (HD == 256 ? 2 : HD == 128 ? 3 : 4);
+  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : HD == 128 ? 2 : 1) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : 3) : (HD == 256 ? 2 : HD == 128 ? 3 : 4);
 }
 template <int TYPE, int HD>
 struct KvBlock {           // one lane's share of a block of 32 keys
@@ -1009,7 +1009,7 @@ hipError_t stream_hd(const PagedAttnArgs& a, hipStream_t s) {
   switch (a.p.hd) {
     case 64: return stream_launch<TYPE, 64>(a, s);
     case 128: return stream_launch<TYPE, 128>(a, s);
-    case 256: if constexpr (TYPE != VLA_KV_F32) return stream_launch<TYPE, 256>(a, s);
+    case 256: if constexpr (TYPE != VLA_KV_BF16) return stream_launch<TYPE, 256>(a, s);   // (bf16: tiles, see the plan)
   }
   return hipErrorInvalidValue;
 }
@@ -1082,7 +1082,8 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((rows + 3) / 4));
   if (a.p.type == VLA_KV_F32) {
     if (a.p.hd == 64) hipLaunchKernelGGL((paged_join<1, 64>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_join<1, 128>), grid, dim3(256), 0, s, a);
+    else if (a.p.hd == 128) hipLaunchKernelGGL((paged_join<1, 128>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join<1, 256>), grid, dim3(256), 0, s, a);
   } else {
     if (a.p.hd == 64) hipLaunchKernelGGL((paged_join<0, 64>), grid, dim3(256), 0, s, a);
     else if (a.p.hd == 128) hipLaunchKernelGGL((paged_join<0, 128>), grid, dim3(256), 0, s, a);

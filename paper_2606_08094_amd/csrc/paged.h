@@ -1,5 +1,5 @@
-// What the kernels on the paged K/V cache share: which request a new token
-// belongs to, which page holds a row, and the 8-bit codes of a page.
+// What the kernels on the paged K/V cache share: which page holds a row, and
+// the 8-bit codes of a page.
 #pragma once
 #include <type_traits>
 
@@ -7,20 +7,6 @@
 #include "vla.h"
 
 constexpr int type_bytes(int type) { return type == VLA_KV_F32 ? 4 : type == VLA_KV_BF16 ? 2 : 1; }
-
-// Largest request b whose first entry key(b) = starts[b] is at most t: the one
-// that token t belongs to, if t is below its end (requests without new tokens
-// share their start with the next one, which wins).  In 0 .. B-1 always.  The
-// lanes of a wave may ask for different tokens.
-VLA_DEV int request_of(const PageArgs& p, int t) {
-  int lo = 0, hi = p.B;            // the answer is in [lo, hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.starts[mid] <= t) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
 
 // Page of row j of request b, or -1: outside the page table, or not in the pool.
 VLA_DEV int page_of(const PageArgs& p, int b, long long j) {

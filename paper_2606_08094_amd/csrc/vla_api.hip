@@ -1692,7 +1692,6 @@ vla_status serve_buffers(const PageArgs& a, bool starts) {
 // The attention's arguments that its plan depends on.
 vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, long long window, PagedAttnArgs* a) {
   VLA_TRY(serve_sizes(pages, batch, &a->p));
-  if (a->p.type == VLA_KV_F32 && a->p.hd == 256) return fail(VLA_E_UNSUPPORTED, "attention over fp32 pages: head_dim 64 or 128");
   if (n_heads < 1 || n_heads % a->p.G) return fail(VLA_E_SHAPE, "n_heads %d is not a multiple of %d K/V heads", n_heads, a->p.G);
   a->H = n_heads;
   a->R = n_heads / a->p.G;

@@ -157,13 +157,6 @@ def test_paged_attention_refusals(vla, change, want):
     assert status(vla, got) == want, vla.lib().vla_last_error()
 
 
-def test_attention_over_fp32_pages_of_256_is_refused(vla):
-    p, b = structs(vla, dict(type=0, head_dim=256), {})
-    L = vla.lib()
-    assert L.vla_paged_attention_workspace(p, b, 2) == ctypes.c_size_t(-1).value
-    assert status(vla, L.vla_paged_attention(p, b, 2, 0, 16, 512, 16, 512, 1.0, 0, 0, None, 16, 1 << 40, None)) == "VLA_E_UNSUPPORTED"
-
-
 def test_paged_attention_workspace_is_checked(vla):
     p, b = structs(vla, {}, dict(max_len=64 * 1024, max_pages=4096))
     L = vla.lib()
