@@ -244,11 +244,13 @@ __global__ __launch_bounds__(64 * SKW) void int8_skinny(Int8Args a) {
 // of eight separate shares would set the pace.
 __device__ const v4u kZero16 = {0, 0, 0, 0};
 
-template <int MR, int NS, int KG>
+template <int MR, int NS, int KG, bool PAIR>
 struct I8Tile {
   static constexpr int BM = 16 * MR, BN = 32 * NS, ROWS = BM + BN;
   static constexpr int SB = ROWS * 8;                                // 16-byte slots per stage
-  static constexpr int NST = std::min(4, 144 * 1024 / (SB * 16 * KG));
+  // PAIR: two stages only, so that two workgroups share a compute unit and one
+  // computes while the other begins or writes its output.
+  static constexpr int NST = PAIR ? 2 : std::min(4, 144 * 1024 / (SB * 16 * KG));
   static constexpr int WV = 8 / KG, WN = WV / 2;                     // waves of a group, along N (two along M)
   static constexpr int MSW = MR / 2, NSW = 2 * NS / WN;              // 16-row subtiles of a wave
   static constexpr int LPT = ROWS / 8 / WV;                          // load instructions of a wave per slice
@@ -323,9 +325,9 @@ VLA_DEV void tile_out(const Int8Args& a, const i32x4 (&acc)[R::MSW][R::NSW], v4u
   }
 }
 
-template <int MR, int NS, int KG>
-__global__ __launch_bounds__(512) void int8_tile(Int8Args a) {
-  using R = I8Tile<MR, NS, KG>;
+template <int MR, int NS, int KG, bool PAIR>
+__global__ __launch_bounds__(512, PAIR ? 4 : 2) void int8_tile(Int8Args a) {
+  using R = I8Tile<MR, NS, KG, PAIR>;
   constexpr int BM = R::BM, BN = R::BN, SB = R::SB, NST = R::NST, D = NST - 1, LPT = R::LPT, MSW = R::MSW, NSW = R::NSW;
   __shared__ v4u ring[KG][NST][SB];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -435,12 +437,12 @@ __global__ __launch_bounds__(512) void int8_tile(Int8Args a) {
   else tile_out<bf16_t, R>(a, acc, &ring[0][0][0], m0, n0, wm, wn, grp == 0);
 }
 
-template <int MR, int NS, int KG>
+template <int MR, int NS, int KG, bool PAIR>
 void tile_launch(Int8Args a, hipStream_t s) {
   a.m_tiles = (a.M + 16 * MR - 1) / (16 * MR);
   a.n_tiles = (a.N + 32 * NS - 1) / (32 * NS);
   const int tiles = a.m_tiles * a.n_tiles;
-  hipLaunchKernelGGL((int8_tile<MR, NS, KG>), dim3((tiles + 7) / 8 * 8), dim3(512), 0, s, a);
+  hipLaunchKernelGGL((int8_tile<MR, NS, KG, PAIR>), dim3((tiles + 7) / 8 * 8), dim3(512), 0, s, a);
 }
 
 template <int MS, int NSUB>
@@ -465,15 +467,24 @@ hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s) {
   // 256) to 71 GB/s (64 x 128), so large tiles win where they fill the chip
   // (816 x 16384 x 2048: 33.7 us, 46.4 us on 128 x 128) and small ones where
   // they would not (816 x 2048 x 16384: 44 us on 64 x 128, 179 us on 256 x 256).
-  struct Cost { int bm, bn; float slice, round; void (*launch)(Int8Args, hipStream_t); };
-  static const Cost costs[] = {{256, 256, 1.50f, 9.8f, tile_launch<16, 8, 1>}, {128, 256, 0.88f, 7.3f, tile_launch<8, 8, 1>},
-                               {128, 128, 0.57f, 4.5f, tile_launch<8, 4, 1>},  {64, 128, 0.34f, 3.2f, tile_launch<4, 4, 2>},
-                               {64, 64, 0.24f, 2.3f, tile_launch<4, 2, 2>}};
+  // Where there are more than 256 tiles of 128 x 128, two of their workgroups can
+  // share a unit, and a last round may be half a one (8192 x 16384 x 1024: 222 us,
+  // 290 one at a time; 1000 x 5000 x 8192: 51 us, 59 on 128 x 256).  Not for rows
+  // that do not begin with a cache line: the smaller the tile, the more lines
+  // they touch in vain (5000 x 2000 x 6000: 103 us, 79 on 256 x 256).
+  struct Cost { int bm, bn; bool pair; float slice, round; void (*launch)(Int8Args, hipStream_t); };
+  static const Cost costs[] = {
+      {256, 256, false, 1.50f, 9.8f, tile_launch<16, 8, 1, false>}, {128, 256, false, 0.88f, 7.3f, tile_launch<8, 8, 1, false>},
+      {128, 128, false, 0.57f, 4.5f, tile_launch<8, 4, 1, false>},  {128, 128, true, 0.51f, 3.0f, tile_launch<8, 4, 1, true>},
+      {64, 128, false, 0.34f, 3.2f, tile_launch<4, 4, 2, false>},   {64, 64, false, 0.24f, 2.3f, tile_launch<4, 2, 2, false>}};
+  const bool lines = a.ldx % 128 == 0 && a.ldw % 128 == 0;
   const Cost* best = nullptr;
   float least = 0.0f;
   for (const Cost& c : costs) {
     const long long tiles = ((a.M + c.bm - 1LL) / c.bm) * ((a.N + c.bn - 1LL) / c.bn);
-    const float t = (float)((tiles + 255) / 256) * ((float)((a.K + 127) / 128) * c.slice + c.round);
+    if (c.pair && (tiles <= 256 || !lines)) continue;
+    const float rounds = c.pair ? 0.5f * (float)((tiles + 127) / 128) : (float)((tiles + 255) / 256);
+    const float t = rounds * ((float)((a.K + 127) / 128) * c.slice + c.round);
     if (!best || t < least) best = &c, least = t;
   }
   // Up to 64 tokens the skinny kernel, which spreads K, is ahead where there are
