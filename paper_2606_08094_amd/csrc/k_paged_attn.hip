@@ -11,6 +11,7 @@
 // group g (= lane / 16) ends up with keys 8 g .. 8 g + 7, which are the k
 // slots of its B operand P^T in O^T += V^T P^T.
 #include <algorithm>
+#include <cmath>
 
 #include "paged.h"
 
@@ -613,9 +614,10 @@ __global__ __launch_bounds__(64 * NW, OCC) void paged_tile(PagedAttnArgs a) {
   const int units = a.slots * p.G * a.nsplit;
   int u = a.by_xcd ? (int)(blockIdx.x % 8u) * (int)(gridDim.x / 8u) + (int)(blockIdx.x / 8u) : (int)blockIdx.x;
   if (u >= units) return;
-  const int slot = u % a.slots;
-  u /= a.slots;
-  const int split = u % a.nsplit, g = u / a.nsplit;
+  const int inner = a.by_xcd ? a.slots : p.G, i0 = u % inner;
+  u /= inner;
+  const int split = u % a.nsplit, outer = u / a.nsplit;
+  const int slot = a.by_xcd ? i0 : outer, g = a.by_xcd ? outer : i0;
   Tile t;
   if (!paged_tile_of<S::ROWS>(a, slot, t)) return;
   int k_lo, k_hi;
@@ -1046,19 +1048,30 @@ void paged_attention_plan(PagedAttnArgs& a, long long span) {
     // two rounds).
     n = std::min(fit / base, (span + 63) / 64);
   } else {
-    // Four rounds, so that long and short requests even out (three prompts of up
-    // to 10007 rows, 715 tiles: 643 us whole, 563 in three splits), as long as
-    // the splits' outputs, written and read in fp32 (about 5 TB/s), take no more
-    // than 15% of the time of the blocks (about 2 us for 64 keys).
-    const double work = (double)base * (span / 64.0) * 2e-6 / fit, outputs = (double)rows * G * a.p.hd * 8 / 5e12;
-    n = std::min((4 * fit + base - 1) / base, (long long)(0.15 * work / std::max(outputs, 1e-12)));
+    // The splits of least estimated time: rounds of the workgroups that fit, of
+    // 2.5 us for 64 keys of 128, and the splits' outputs, written and read in fp32
+    // (about 5 TB/s).  The tiles of one request are alike and take whole rounds
+    // (2048 tokens over 8192 rows, 325 tiles: 321 us whole, 294 in two splits, 236
+    // in three, 263 in four); of several, some 70% of the tiles' keys are there,
+    // and half a round passes at the end (three prompts of up to 10007 rows, 715
+    // tiles: 600 us whole, 520 in three or four; 32 of 500 tokens over 2000 rows:
+    // 210 whole, 272 in two).
+    const double tile_us = (span / 64.0) * 2.5 * a.p.hd / 128, out_us = (double)rows * G * a.p.hd * 8 / 5e6;
+    double least = 0.0;
+    n = 1;
+    for (int k = 1; k <= 8; ++k) {
+      const double load = (double)base * k / fit, rounds = B == 1 ? std::ceil(load) : std::max(1.0, 0.7 * load + 0.5);
+      const double us = rounds * tile_us / k + (k > 1 ? k * out_us : 0.0);
+      if (k == 1 || us < least) n = k, least = us;
+    }
   }
   a.nsplit = (int)std::max(1LL, std::min(n, 64LL));
-  // Consecutive tiles on one XCD read the same keys through its L2; in many
-  // rounds tiles of unequal length had better go to all XCDs in turn (4 x 600
-  // tokens over 4000 keys, one round: 95 us against 102; three prompts of up to
-  // 10007 rows: 560 us against 545).
-  a.by_xcd = base * a.nsplit <= 2 * fit;
+  // Tile kernel: consecutive tiles on one XCD read the same keys through its L2
+  // (4 x 600 tokens over 4000 keys: 95 us, in turn over all XCDs 102).  In more
+  // rounds, or more than one of whole tiles, which differ most in length, all
+  // heads of the first requests go first, in turn over all XCDs (8 x 800 tokens
+  // over 866 rows of 256: 146 us against 125; 6 x 1000 over 4000: 243, 220).
+  a.by_xcd = a.nsplit > 1 ? base * a.nsplit <= 2 * fit : base <= fit;
   a.chunk = (int)((span + a.nsplit - 1) / a.nsplit + 31) & ~31;
   if (a.chunk < 32) a.chunk = 32;
 }

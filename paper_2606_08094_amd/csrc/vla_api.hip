@@ -1801,7 +1801,8 @@ vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* ba
   if (a.p.T == 0 || a.p.B == 0) return VLA_OK;
   VLA_TRY(serve_buffers(a.p, true));
   if (!q || !o || !al16(q) || !al16(o) || !al16(lse)) return fail(VLA_E_ARG, "q and o must be non-NULL, q, o and lse 16-byte aligned");
-  const size_t need = vla_paged_attention_workspace(pages, batch, n_heads);
+  // (a shorter span takes no more splits, so this is what the function says)
+  const size_t need = std::max(vla_paged_attention_workspace(pages, batch, n_heads), paged_attention_bytes(a));
   if (workspace_bytes < need) return fail(VLA_E_SHAPE, "workspace_bytes %zu < %zu", workspace_bytes, need);
   if (need && (!workspace || !al16(workspace))) return fail(VLA_E_ARG, "workspace must be non-NULL and 16-byte aligned");
   a.causal = causal; a.q = q; a.ldq = ldq; a.o = o; a.ldo = ldo; a.lse = lse; a.scale = scale;
