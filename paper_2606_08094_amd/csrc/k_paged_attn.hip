@@ -105,7 +105,8 @@ VLA_DEV void tile_keys(const PagedAttnArgs& a, const Tile& t, int rows, int spli
   const int span = max(hi - lo, 0);
   const int ns = min((span + a.chunk - 1) / a.chunk, a.nsplit);
   int each = ns > 0 ? (span + ns - 1) / ns : 0;
-  each = each > 64 ? (each + 127) & ~127 : (each + 31) & ~31;   // whole rounds of four waves, or one or two waves
+  if (rows > 16) each = (each + 63) & ~63;                    // blocks of the tile kernel
+  else each = each > 64 ? (each + 127) & ~127 : (each + 31) & ~31;   // whole rounds of four waves, or one or two waves
   if (split >= ns) {
     hi = lo;
     return;
@@ -1042,26 +1043,27 @@ void paged_attention_plan(PagedAttnArgs& a, long long span) {
     // is done before a second launch would be (72 rows of fp32: 7.0 us, 9.6 in
     // three splits).
     n = span <= 256 ? 1 : std::max(std::min((1536 + base - 1) / base, (span + 95) / 96), std::min(256 / base, (span + 31) / 32));
-  } else if (2 * base <= fit) {
-    // One round of the workgroups that fit the chip (8 x 50 tokens of 8 heads
-    // over 866 rows of 256: 36 us whole, 23 in 5 to 7 splits, 31 in 8, which are
-    // two rounds).
-    n = std::min(fit / base, (span + 63) / 64);
   } else {
-    // The splits of least estimated time: rounds of the workgroups that fit, of
-    // 2.5 us for 64 keys of 128, and the splits' outputs, written and read in fp32
-    // (about 5 TB/s).  The tiles of one request are alike and take whole rounds
-    // (2048 tokens over 8192 rows, 325 tiles: 321 us whole, 294 in two splits, 236
-    // in three, 263 in four); of several, some 70% of the tiles' keys are there,
-    // and half a round passes at the end (three prompts of up to 10007 rows, 715
-    // tiles: 600 us whole, 520 in three or four; 32 of 500 tokens over 2000 rows:
-    // 210 whole, 272 in two).
-    const double tile_us = (span / 64.0) * 2.5 * a.p.hd / 128, out_us = (double)rows * G * a.p.hd * 8 / 5e6;
+    // The splits of least estimated time: rounds of the workgroups that fit, each
+    // of its blocks of 64 keys (measured: 1.75, 2.5, 3 us at 64, 128, 256) and what
+    // it begins and ends with, then the splits' outputs, written and read in fp32
+    // (about 5 TB/s), and a launch.  The tiles of one request are alike and take
+    // whole rounds (2048 tokens over 8192 rows, 325 tiles: 321 us whole, 294 in two
+    // splits, 236 in three, 263 in four); of several, some 75% of the tiles' keys
+    // are there, and half a round passes at the end (three prompts of up to 10007
+    // rows, 715 tiles: 600 us whole, 520 in three or four; 24 of 21 tokens over 9787
+    // rows of 64: 265 whole, 151 in two, 98 in eight; 8 x 50 tokens of 8 heads over
+    // 866 rows of 256: 36 whole, 23 in five to seven, 31 in eight).
+    const double tile_us = (span / 64.0) * (a.p.hd == 64 ? 1.75 : a.p.hd == 128 ? 2.5 : 3.0), ends_us = a.p.hd == 256 ? 6.0 : 2.0;
+    const double out_us = (double)rows * G * a.p.hd * 8 / 5e6;
+    const double tiles_of_all = std::max((double)B, rows / 128.0 + 0.5 * B) * G;   // (a tile slot may be empty)
+    const long long most = std::min({std::max(8LL, fit / base), (span + 63) / 64, 64LL});
     double least = 0.0;
     n = 1;
-    for (int k = 1; k <= 8; ++k) {
-      const double load = (double)base * k / fit, rounds = B == 1 ? std::ceil(load) : std::max(1.0, 0.7 * load + 0.5);
-      const double us = rounds * tile_us / k + (k > 1 ? k * out_us : 0.0);
+    for (long long k = 1; k <= most; ++k) {
+      const double load = tiles_of_all * k / fit;
+      const double rounds = load <= 1.0 ? 1.0 : B == 1 ? std::ceil(load) : 0.75 * load + 0.5;
+      const double us = rounds * (tile_us / k + ends_us) + (k > 1 ? k * out_us + 3.0 : 0.0);
       if (k == 1 || us < least) n = k, least = us;
     }
   }
