@@ -491,7 +491,7 @@ hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s) {
   // few columns (a workgroup takes in about 36 GB/s of its rows of W and the
   // tokens'): 36 x 20 x 13120 in 16 us, 1 x 2560 x 2560 in 4.4, but 64 x 16384 x
   // 8192 in 60 us against 32 on tiles.
-  const bool two = a.N >= 16 * 2 * 256;
+  const bool two = a.N >= 16 * 2 * 256 && a.M <= 32;
   const float wide = two ? 32.0f : 16.0f, rounds = (float)(((long long)(a.N + (int)wide - 1) / (int)wide + 255) / 256);
   if (a.M <= 64 && rounds * (wide + (float)a.M) * (float)a.K / 36e3f + 3.0f < least) {
     switch ((a.M <= 16 ? 10 : a.M <= 32 ? 20 : 40) + two) {
@@ -499,8 +499,7 @@ hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s) {
       case 11: skinny_launch<1, 2>(a, s); break;
       case 20: skinny_launch<2, 1>(a, s); break;
       case 21: skinny_launch<2, 2>(a, s); break;
-      case 40: skinny_launch<4, 1>(a, s); break;
-      default: skinny_launch<4, 2>(a, s); break;
+      default: skinny_launch<4, 1>(a, s); break;
     }
   } else {
     best->launch(a, s);

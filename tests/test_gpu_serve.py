@@ -41,6 +41,7 @@ def host(t):
 @pytest.mark.parametrize("M,K,pad_x,pad_q", [
     (1, 0, 0, 0), (1, 1, 0, 0), (3, 7, 1, 2), (1, 16, 0, 0), (5, 64, 8, 16), (50, 720, 0, 0), (7, 1023, 1, 1), (2, 2048, 0, 0),
     (3, 2056, 0, 8), (4, 2560, 0, 0), (2, 6912, 8, 0), (1, 16384, 0, 0), (2, 16392, 0, 0), (2, 40000, 0, 0), (257, 64, 0, 0),
+    (1027, 200, 0, 0), (1025, 1032, 0, 8), (1030, 2056, 8, 0), (1025, 4104, 0, 0),      # a wave per row
 ])
 def test_quantize_tokens(torch, vla, elem, M, K, pad_x, pad_q):
     rng = np.random.default_rng(M * 1000 + K)
@@ -78,6 +79,9 @@ GEMM = [  # M, N, K, extra pitch of q, w, y
     (65, 257, 144, 0, 0, 0), (128, 256, 256, 0, 0, 0), (129, 255, 272, 0, 0, 0), (241, 1601, 720, 0, 0, 0), (256, 256, 64, 0, 0, 8),
     (257, 513, 1040, 16, 32, 0), (400, 720, 960, 0, 0, 0), (816, 512, 2048, 0, 0, 0), (2, 3, 0, 0, 0, 0), (300, 70, 0, 0, 0, 0),
     (1000, 96, 4096, 0, 0, 0), (37, 2000, 131056, 0, 0, 0), (700, 1300, 16, 0, 0, 0),
+    (20, 300, 1040, 0, 0, 0), (33, 70, 4096, 16, 0, 1), (3, 8200, 2048, 0, 0, 0), (17, 8199, 3008, 0, 0, 0),   # few tokens
+    (816, 2050, 528, 0, 0, 0), (1100, 1500, 2048, 0, 16, 0), (1000, 3000, 1040, 0, 0, 0), (1030, 2100, 528, 0, 0, 4),   # and
+    (2049, 2050, 256, 0, 0, 0), (2100, 2100, 80, 0, 0, 0), (1500, 4100, 144, 16, 0, 0), (4100, 4100, 272, 0, 0, 0),     # tiles
 ]
 
 
@@ -239,6 +243,13 @@ def test_write_and_read_back(torch, vla, kind, source, hd, G, page, lens):
         few = torch.full((len(lens), G, 1, hd), 3.25, dtype=out[0].dtype, device="cuda")   # fewer rows than there are
         vla.kv_pages_read(P.pages, P.batch(), 1, vla.ELEMS[elem], few, few.clone())
         assert np.array_equal(host(few), host(out[0][:, :, :1]))
+
+
+@pytest.mark.parametrize("kind,source", [("i8", "bf16"), ("e4m3", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("hd,G,page,lens", [(64, 4, 256, [3001, 1, 0, 1100]), (64, 4, 64, [9000, 17, 7500]), (128, 2, 16, [1, 8300])])
+def test_write_and_read_back_many_rows(torch, vla, kind, source, hd, G, page, lens):
+    """As many rows as are written several to a wave."""
+    test_write_and_read_back(torch, vla, kind, source, hd, G, page, lens)
 
 
 def test_write_ties_zeros_and_rows_that_are_not_finite(torch, vla):
@@ -421,6 +432,7 @@ def test_paged_attention_many_requests(torch, vla, kind):
     (128, 8, 1, [3000, 40, 5000, 1], [1, 1, 1, 1]),        # one token each, the keys in many splits
     (256, 1, 8, [4000, 500], [1, 3]),
     (128, 1, 4, [9000], [40]),                             # one round of tiles, the keys in many splits
+    (64, 5, 8, [4000, 700, 2500, 1, 900, 3100], [21, 3, 12, 1, 20, 7]),     # few rows each, more than a round of splits
 ])
 def test_paged_attention_at_size(torch, vla, kind, hd, G, R, lens, news):
     """The shapes whose work is spread in other ways; some heads of each."""
