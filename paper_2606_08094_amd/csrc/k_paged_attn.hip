@@ -251,25 +251,48 @@ VLA_DEV void add_not_finite(const PageArgs& p, const int* table, int g, int k0, 
 
 // ---------------------------------------------------------------------------
 // paged_stream: a tile of 16 rows per workgroup, the keys of a split dealt to
-// four waves in blocks of 32.  K goes straight from memory into the MFMA A
-// operand.  So does V: lane group g loads keys 8 g .. 8 g + 7, each lane the
-// same dimensions of all eight, so the V^T operand (eight keys of a dimension)
-// is a permutation of the lane's own registers; which of the head's dimensions
-// a row of an O^T tile stands for is free.  No LDS until the waves' results
-// are joined, no barrier among the loads.
+// four waves in blocks of 32.  V goes straight from memory into the MFMA A
+// operand: lane group g loads keys 8 g .. 8 g + 7, each lane the same dimensions
+// of all eight, so the V^T operand (eight keys of a dimension) is a permutation
+// of the lane's own registers; which of the head's dimensions a row of an O^T
+// tile stands for is free.  K goes by way of LDS, or directly (see KRows).  No
+// barrier until the waves' results are joined.
 //
-// Bound by the cache's bytes.  A block's K and V are all in flight before the
-// first is used, and the page ids of the next one; the waves of a SIMD hide
-// each other's waits (a second block in flight per wave leaves room for half
-// the waves: 64 requests of up to 8192 rows of int8, 117 us instead of 113).
-// Loads have no branches: a key that does not exist is read from page 0 and
-// not used.
+// Bound by the cache's bytes: with the arithmetic taken out it takes the same
+// time.  The waves of a SIMD hide each other's waits (a second block of both in
+// flight per wave leaves room for half the waves: 64 requests of up to 8192 rows
+// of int8, 117 us instead of 113 at the time).  Loads have no branches: a key
+// that does not exist is read from page 0 and not used.
 // Workgroups per compute unit that the registers have to allow: as many as
 // they do without spilling.
 template <int TYPE, int HD>
 constexpr int stream_occupancy() {
   return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : HD == 128 ? 2 : 1) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : 3) : (HD == 256 ? 2 : HD == 128 ? 3 : 4);
 }
+// K by way of LDS.  A K operand has sixteen rows in sixteen neighbouring lanes, so
+// a load straight into it touches a cache line per lane (some 40 per load
+// instruction, and their number is what the cache keeps up with).  Instead whole
+// rows go to LDS by direct loads, piece c (16 bytes) of row `key` at slot
+// c ^ slot(key), so that the sixteen rows of an operand read lie in different
+// banks.  The next block's are under way while a block is worked on.  64 requests
+// of up to 8192 rows of 128: int8 96.0 -> 93.0 us, bf16 161 -> 150; fp32, 22 x 50
+// tokens over 9737 rows of 128: 345 -> 297.  Not where it does not pay: rows of 64
+// bytes, of which four lanes read all (54 us, 57 by LDS), fp32 rows of 256, whose
+// registers are full (180, 203), and of 64 (the same at size, a short call 0.2 us
+// more).
+// A wave's share of LDS also takes its outputs in the end.
+template <int TYPE, int HD>
+struct KRows {
+  static constexpr int RB = HD * type_bytes(TYPE), VPR = RB / 16;   // bytes and pieces of a row
+  static constexpr bool USED = TYPE == VLA_KV_F32 ? HD == 128 : RB >= 128;
+  static constexpr int RPI = 64 / VPR, NI = 32 / RPI;               // rows of a load, loads of a block
+  static constexpr int BYTES = std::max(USED ? 32 * RB : 0, HD / 16 * 1024);
+  static VLA_DEV int slot(int key) {
+    if constexpr (VPR == 8) return key >> 3 | (key & 2) << 1;
+    else return key >> 3 | (key & 3) << 2;
+  }
+};
+
 template <int TYPE, int HD>
 struct KvBlock {           // one lane's share of a block of 32 keys
   using L = Lay<TYPE, HD>;
@@ -284,7 +307,8 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
   using L = Lay<TYPE, HD>;
   using E = std::conditional_t<L::F32, float, bf16_t>;
   constexpr int DT = L::DT, VE = L::VE, NH = L::NH, W = 4;
-  __shared__ float so[W][DT][64][4];
+  using KR = KRows<TYPE, HD>;
+  __shared__ __align__(16) unsigned char lds[W][KR::BYTES];
   __shared__ float sm[W][16], sl[W][16];
 
   const PageArgs& p = a.p;
@@ -311,17 +335,29 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
     kp = kk < k_hi ? table[kk >> p.lg] : -1;
     vp = vk < k_hi ? table[vk >> p.lg] : -1;
   };
-  auto load = [&](int kb, int kp, int vp, KvBlock<TYPE, HD>& x) {
-    const size_t kpid = (unsigned)kp < (unsigned)p.n_pages ? kp : 0;
-    x.vpid = (unsigned)vp < (unsigned)p.n_pages ? vp : -1;
-    const size_t krow = (kpid * p.G + g) * pagerows + ((kb + 8 * (r16 >> 2)) & mask) + (r16 & 3);
-    const size_t vrow = ((size_t)max(x.vpid, 0) * p.G + g) * pagerows + ((kb + 8 * g4) & mask);
+  unsigned char* const mine = lds[wave];
+  auto issue_k = [&](int kb, int kp) {          // K rows of a block on their way into LDS
+    const int p0 = __builtin_amdgcn_readlane(kp, 0), p1 = __builtin_amdgcn_readlane(kp, 8);   // its halves' pages
+#pragma unroll
+    for (int j = 0; j < KR::NI; ++j) {
+      const int r = j * KR::RPI, key = r + lane / KR::VPR, p16 = r < 16 ? p0 : p1;
+      const size_t row = ((size_t)((unsigned)p16 < (unsigned)p.n_pages ? p16 : 0) * p.G + g) * pagerows + ((kb + r) & mask);
+      const char* src = reinterpret_cast<const char*>(p.k) + row * KR::RB + lane / KR::VPR * KR::RB + 16 * (lane % KR::VPR ^ KR::slot(key));
+      dma16(src, reinterpret_cast<v4u*>(mine + 1024 * j));
+    }
+  };
+  auto load_k = [&](int kb, int kp, KvBlock<TYPE, HD>& x) {
+    const size_t krow = ((size_t)((unsigned)kp < (unsigned)p.n_pages ? kp : 0) * p.G + g) * pagerows + ((kb + 8 * (r16 >> 2)) & mask) + (r16 & 3);
     const char* ka = reinterpret_cast<const char*>(p.k) + krow * (HD * L::ES) + 16 * g4;
-    const char* va = reinterpret_cast<const char*>(p.v) + vrow * (HD * L::ES) + r16 * L::VB;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int c = 0; c < L::NK; ++c) x.k[tt][c] = ldg16(ka + tt * 4 * (HD * L::ES) + 64 * c);
+  };
+  auto load_v = [&](int kb, int vp, KvBlock<TYPE, HD>& x) {   // and the scales
+    x.vpid = (unsigned)vp < (unsigned)p.n_pages ? vp : -1;
+    const size_t vrow = ((size_t)max(x.vpid, 0) * p.G + g) * pagerows + ((kb + 8 * g4) & mask);
+    const char* va = reinterpret_cast<const char*>(p.v) + vrow * (HD * L::ES) + r16 * L::VB;
     if constexpr (L::ES == 1) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -337,8 +373,12 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
   constexpr int STEP = 32 * W;
   const int kb0 = k_lo + 32 * wave;
   KvBlock<TYPE, HD> buf;
-  int kp = -1, vp = -1;
+  int kp = -1, vp = -1, kp1 = -1, vp1 = -1;     // pages of this block and (K by LDS) of the next one
   pids(kb0, kp, vp);
+  if constexpr (KR::USED) {
+    pids(kb0 + STEP, kp1, vp1);
+    if (kb0 < k_hi) issue_k(kb0, kp);
+  }
 
   // this lane's row of the tile
   const int rr = t.row0 + r16;
@@ -488,8 +528,28 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
   };
 
   for (int kb = kb0; kb < k_hi; kb += STEP) {
-    load(kb, kp, vp, buf);
-    pids(kb + STEP, kp, vp);
+    if constexpr (KR::USED) {
+      // This block's K rows have landed: they were loaded before the last block's V.
+      __builtin_amdgcn_s_waitcnt(vm_wait(0));
+      asm volatile("" : : : "memory");
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int c = 0; c < L::NK; ++c) {
+          const int key = 8 * (r16 >> 2) + 4 * tt + (r16 & 3);
+          buf.k[tt][c] = *reinterpret_cast<const uint4*>(mine + key * KR::RB + 16 * ((4 * c + g4) ^ KR::slot(key)));
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // before the next ones overwrite them
+      if (kb + STEP < k_hi) issue_k(kb + STEP, kp1);
+      const int vnow = vp;
+      vp = vp1;
+      pids(kb + 2 * STEP, kp1, vp1);
+      load_v(kb, vnow, buf);
+    } else {
+      load_k(kb, kp, buf);
+      load_v(kb, vp, buf);
+      pids(kb + STEP, kp, vp);
+    }
     block(kb, buf);
   }
 
@@ -511,7 +571,7 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
   }
   if (wave < nact) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(so[wave][d][lane]) = o[d];
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(mine + 1024 * d + 16 * lane) = o[d];
   }
   __syncthreads();
   float mx = -INFINITY;
@@ -542,7 +602,7 @@ __global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_str
     v[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < W; ++w)
-      if (w < nact) v[d] += *reinterpret_cast<const f32x4*>(so[w][d0 + d][lane]) * f[w];
+      if (w < nact) v[d] += *reinterpret_cast<const f32x4*>(lds[w] + 1024 * (d0 + d) + 16 * lane) * f[w];
     v[d] *= inv;
   }
   float* pd = a.part + ((size_t)split * p.T * a.H + th) * HD + dim0;
