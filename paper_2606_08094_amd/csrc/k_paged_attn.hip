@@ -265,9 +265,8 @@ VLA_DEV void add_not_finite(const PageArgs& p, const int* table, int g, int k0, 
 // that does not exist is read from page 0 and not used.
 // Workgroups per compute unit that the registers have to allow: as many as
 // they do without spilling.
-template <int TYPE, int HD>
-constexpr int stream_occupancy() {
-  return TYPE == VLA_KV_F32 ? (HD == 64 ? 3 : HD == 128 ? 2 : 1) : TYPE == VLA_KV_BF16 ? (HD == 64 ? 4 : 3) : (HD == 256 ? 2 : HD == 128 ? 3 : 4);
+constexpr int stream_occupancy(int type, int hd) {
+  return type == VLA_KV_F32 ? (hd == 64 ? 3 : hd == 128 ? 2 : 1) : type == VLA_KV_BF16 ? (hd == 64 ? 4 : 3) : (hd == 256 ? 2 : hd == 128 ? 3 : 4);
 }
 // K by way of LDS.  A K operand has sixteen rows in sixteen neighbouring lanes, so
 // a load straight into it touches a cache line per lane (some 40 per load
@@ -303,7 +302,7 @@ struct KvBlock {           // one lane's share of a block of 32 keys
 };
 
 template <int TYPE, int HD>
-__global__ __launch_bounds__(256, (stream_occupancy<TYPE, HD>())) void paged_stream(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, stream_occupancy(TYPE, HD)) void paged_stream(PagedAttnArgs a) {
   using L = Lay<TYPE, HD>;
   using E = std::conditional_t<L::F32, float, bf16_t>;
   constexpr int DT = L::DT, VE = L::VE, NH = L::NH, W = 4;
@@ -1079,7 +1078,12 @@ hipError_t stream_hd(const PagedAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-void paged_attention_plan(PagedAttnArgs& a, long long span) {
+// The split counts that are tried: all up to 8, then in steps of a fourth, and the last.
+static long long next_split(long long k, long long end) {
+  return k == end ? end + 1 : std::min(end, k + (k < 8 ? 1 : k / 4));
+}
+
+void paged_attention_plan(PagedAttnArgs& a, long long span, int most) {
   a.rdiv = ((1ull << 32) + a.R - 1) / a.R;
   const long long rows = (long long)a.p.T * a.R, B = std::max(1, a.p.B), G = a.p.G;
   // The 128-row tile reads a key once for all rows, but a request with few rows
@@ -1096,13 +1100,25 @@ void paged_attention_plan(PagedAttnArgs& a, long long span) {
   const long long base = std::max(1LL, a.slots * G);
   long long n;
   if (!tile) {
-    // About 1536 workgroups of 96 keys or more (64 requests of up to 8192 rows
-    // of int8: 125 us whole, 95 in 4 splits, 124 in 32), or a workgroup per
-    // compute unit with a wave's 32 keys at least: a CU takes in some 50 GB/s,
-    // so a short request is spread wide as well.  Up to 256 rows one workgroup
-    // is done before a second launch would be (72 rows of fp32: 7.0 us, 9.6 in
-    // three splits).
-    n = span <= 256 ? 1 : std::max(std::min((1536 + base - 1) / base, (span + 95) / 96), std::min(256 / base, (span + 31) / 32));
+    // The splits of least estimated time.  A workgroup begins and ends in some 6 us
+    // and takes 0.5 us and its bytes' time for each 128 keys (fp32: its products'
+    // time), one after the other; together they take as long as memory needs, the
+    // longest ones' last third, when they do not fill it any more, and 3.5 us per
+    // workgroup of a full chip; a join is a launch of 6.5 us.  64 requests of up to
+    // 8192 rows of int8: 114 us whole, 93 in four splits, 96 in eight, 130 in 32; one:
+    // 66 whole, 13 in 24; 32 of 1000 rows: 14 whole, 16 in four.
+    const double bytes = a.p.hd * (a.p.type == VLA_KV_BF16 ? 4.0 : a.p.type == VLA_KV_F32 ? 8.0 : 2.0) + (a.p.type >= VLA_KV_I8 ? 8.0 : 0.0);
+    const double chain = span / 128.0 * (a.p.type == VLA_KV_F32 ? a.p.hd * 0.02 : 0.5 + 0.0018 * bytes);
+    const double memory = (B == 1 ? 1.0 : 0.6) * span * B * G * bytes / 4.2e6, out_us = (double)rows * G * a.p.hd * 8 / 5e6;
+    const double fit = 256.0 * stream_occupancy(a.p.type, a.p.hd), units = std::max((double)B, rows / 16.0 + 0.5 * B) * G;
+    const long long end = std::min((span + 31) / 32, (long long)most);
+    double least = 0.0;
+    n = 1;
+    for (long long k = 1; k <= end; k = next_split(k, end)) {
+      const double load = units * k / fit, alone = std::max(1.0, B == 1 ? load : 0.75 * load) * (chain / k + 6.0);
+      const double us = std::max(alone, memory + 0.35 * chain / k + 3.5 * load) + (k > 1 ? 6.5 + k * (0.05 + out_us) : 0.0);
+      if (k == 1 || us < least) n = k, least = us;
+    }
   } else {
     // The splits of least estimated time: rounds of the workgroups that fit, each
     // of its blocks of 64 keys (measured: 1.75, 2.5, 3 us at 64, 128, 256) and what
@@ -1114,20 +1130,22 @@ void paged_attention_plan(PagedAttnArgs& a, long long span) {
     // rows, 715 tiles: 600 us whole, 520 in three or four; 24 of 21 tokens over 9787
     // rows of 64: 265 whole, 151 in two, 98 in eight; 8 x 50 tokens of 8 heads over
     // 866 rows of 256: 36 whole, 23 in five to seven, 31 in eight).
-    const double tile_us = (span / 64.0) * (a.p.hd == 64 ? 1.75 : a.p.hd == 128 ? 2.5 : 3.0), ends_us = a.p.hd == 256 ? 6.0 : 2.0;
+    const double block_us = a.p.hd == 64 ? 1.75 : a.p.hd == 128 ? 2.5 : 3.0, ends_us = a.p.hd == 256 ? 6.0 : 2.0;
     const double out_us = (double)rows * G * a.p.hd * 8 / 5e6;
     const double tiles_of_all = std::max((double)B, rows / 128.0 + 0.5 * B) * G;   // (a tile slot may be empty)
-    const long long most = std::min({std::max(8LL, fit / base), (span + 63) / 64, 64LL});
+    const long long end = std::min({std::max(8LL, fit / base), (span + 63) / 64, (long long)most});
     double least = 0.0;
     n = 1;
-    for (long long k = 1; k <= most; ++k) {
+    const long long blocks = (span + 63) / 64;
+    for (long long t = 1; t <= end; t = next_split(t, end)) {
+      const long long each = (blocks + t - 1) / t, k = each > 0 ? (blocks + each - 1) / each : 1;   // splits of whole blocks
       const double load = tiles_of_all * k / fit;
       const double rounds = load <= 1.0 ? 1.0 : B == 1 ? std::ceil(load) : 0.75 * load + 0.5;
-      const double us = rounds * (tile_us / k + ends_us) + (k > 1 ? k * out_us + 3.0 : 0.0);
-      if (k == 1 || us < least) n = k, least = us;
+      const double us = rounds * (each * block_us + ends_us) + (k > 1 ? k * out_us + 3.0 : 0.0);
+      if (t == 1 || us < least) n = k, least = us;
     }
   }
-  a.nsplit = (int)std::max(1LL, std::min(n, 64LL));
+  a.nsplit = (int)n;
   // Tile kernel: consecutive tiles on one XCD read the same keys through its L2
   // (4 x 600 tokens over 4000 keys: 95 us, in turn over all XCDs 102).  In more
   // rounds, or more than one of whole tiles, which differ most in length, all

@@ -1690,16 +1690,18 @@ vla_status serve_buffers(const PageArgs& a, bool starts) {
 }
 
 // The attention's arguments that its plan depends on.
-vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, long long window, PagedAttnArgs* a) {
+vla_status paged_plan(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, long long window, PagedAttnArgs* a,
+                      size_t* workspace) {
   VLA_TRY(serve_sizes(pages, batch, &a->p));
   if (n_heads < 1 || n_heads % a->p.G) return fail(VLA_E_SHAPE, "n_heads %d is not a multiple of %d K/V heads", n_heads, a->p.G);
   a->H = n_heads;
   a->R = n_heads / a->p.G;
   if (a->R > 16) return fail(VLA_E_UNSUPPORTED, "more than 16 query heads per K/V head");
-  long long span = std::min<long long>(batch->max_len, (long long)batch->max_pages << a->p.lg);
-  if (window > 0) span = std::min(span, window + 1024);
+  const long long span = std::min<long long>(batch->max_len, (long long)batch->max_pages << a->p.lg);
   a->window = window;
-  paged_attention_plan(*a, span);
+  paged_attention_plan(*a, span, 64);
+  *workspace = paged_attention_bytes(*a);     // enough for any window: it takes no more splits
+  if (window > 0 && window + 1024 < span) paged_attention_plan(*a, window + 1024, a->nsplit);
   if ((long long)a->slots * a->p.G * a->nsplit * 512 > kMaxThreads || (long long)a->p.T * a->H * 64 > kMaxThreads)
     return fail(VLA_E_UNSUPPORTED, "too many tokens and heads for one call");
   return VLA_OK;
@@ -1779,8 +1781,9 @@ vla_status vla_kv_pages_read(const vla_kv_pages* pages, const vla_kv_batch* batc
 
 size_t vla_paged_attention_workspace(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads) {
   PagedAttnArgs a{};
-  if (paged_plan(pages, batch, n_heads, 0, &a) != VLA_OK) return (size_t)-1;
-  return paged_attention_bytes(a);
+  size_t need;
+  if (paged_plan(pages, batch, n_heads, 0, &a, &need) != VLA_OK) return (size_t)-1;
+  return need;
 }
 
 vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* batch, int32_t n_heads, int32_t elem,
@@ -1792,7 +1795,8 @@ vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* ba
   if (causal != 0 && causal != 1) return fail(VLA_E_ARG, "causal must be 0 or 1");
   if (!std::isfinite(scale)) return fail(VLA_E_ARG, "scale must be finite");
   PagedAttnArgs a{};
-  VLA_TRY(paged_plan(pages, batch, n_heads, window, &a));
+  size_t need;
+  VLA_TRY(paged_plan(pages, batch, n_heads, window, &a, &need));
   if ((elem == VLA_T_F32) != (a.p.type == VLA_KV_F32))
     return fail(VLA_E_UNSUPPORTED, "fp32 queries go with fp32 pages, bf16 queries with the other types");
   const long long d = (long long)n_heads * a.p.hd;
@@ -1800,11 +1804,9 @@ vla_status vla_paged_attention(const vla_kv_pages* pages, const vla_kv_batch* ba
     return fail(VLA_E_SHAPE, "ldq and ldo must be at least n_heads * head_dim and multiples of 16 bytes");
   if (a.p.T == 0 || a.p.B == 0) return VLA_OK;
   VLA_TRY(serve_buffers(a.p, true));
-  if (!q || !o || !al16(q) || !al16(o) || !al16(lse)) return fail(VLA_E_ARG, "q and o must be non-NULL, q, o and lse 16-byte aligned");
-  // (a shorter span takes no more splits, so this is what the function says)
-  const size_t need = std::max(vla_paged_attention_workspace(pages, batch, n_heads), paged_attention_bytes(a));
   if (workspace_bytes < need) return fail(VLA_E_SHAPE, "workspace_bytes %zu < %zu", workspace_bytes, need);
   if (need && (!workspace || !al16(workspace))) return fail(VLA_E_ARG, "workspace must be non-NULL and 16-byte aligned");
+  if (!q || !o || !al16(q) || !al16(o) || !al16(lse)) return fail(VLA_E_ARG, "q and o must be non-NULL, q, o and lse 16-byte aligned");
   a.causal = causal; a.q = q; a.ldq = ldq; a.o = o; a.ldo = ldo; a.lse = lse; a.scale = scale;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + (size_t)a.nsplit * a.p.T * a.H * a.p.hd;

@@ -374,8 +374,8 @@ hipError_t launch_quantize_tokens(int f32, const QuantTokArgs& a, hipStream_t s)
 hipError_t launch_int8_gemm(const Int8Args& a, hipStream_t s);
 hipError_t launch_pages_write(const PageRowsArgs& a, hipStream_t s);
 hipError_t launch_pages_read(const PageRowsArgs& a, hipStream_t s);
-// Row tiles, splits and split length for these sizes (max_len: the host's
-// bound of the rows of a request; span: rows that a tile of queries may see).
-void paged_attention_plan(PagedAttnArgs& a, long long span);
+// Row tiles, splits (at most `most`) and split length for these sizes; span: the
+// host's idea of the most rows that a tile of queries sees.
+void paged_attention_plan(PagedAttnArgs& a, long long span, int most);
 size_t paged_attention_bytes(const PagedAttnArgs& a);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s);

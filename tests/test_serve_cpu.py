@@ -2,6 +2,7 @@
 can see is turned away before a device is touched (no GPU needed)."""
 import ctypes
 import os
+import random
 
 import pytest
 
@@ -178,6 +179,19 @@ def test_workspace_covers_every_window(vla):
         for window in (0, 1, 31, 1000, 50000, 2 ** 31 - 1):
             got = L.vla_paged_attention(p, b, 4, 1, None, 512, 16, 512, 0.1, 1, window, None, 16, need, None)
             assert status(vla, got) == "VLA_E_ARG" and b"q and o" in L.vla_last_error()
+
+
+def test_workspace_covers_every_window_over_the_sizes(vla):
+    L, rng = vla.lib(), random.Random(5)
+    for _ in range(3000):
+        kind, hd, G, R = rng.randrange(4), rng.choice([64, 128, 256]), rng.choice([1, 2, 5, 8]), rng.choice([1, 3, 8])
+        B = int(2 ** rng.uniform(0, 7))
+        p, b = structs(vla, dict(type=kind, head_dim=hd, n_kv_heads=G, k_scale=16, v_scale=16),
+                       dict(n_requests=B, n_tokens=int(B * 2 ** rng.uniform(0, 10)), max_len=int(2 ** rng.uniform(0, 16)), max_pages=1 << 12))
+        need = L.vla_paged_attention_workspace(p, b, G * R)
+        window, ld, elem = int(2 ** rng.uniform(0, 17)), G * R * hd, 0 if kind == 0 else 1
+        got = L.vla_paged_attention(p, b, G * R, elem, None, ld, 16, ld, 0.1, 1, window, None, 16, need, None)
+        assert status(vla, got) == "VLA_E_ARG" and b"q and o" in L.vla_last_error(), (kind, hd, G, R, B, window)
 
 
 def test_binding_turns_host_tensors_away(vla):
