@@ -348,7 +348,8 @@ vla_status vla_quantize_tokens(int32_t elem, const void* x, int32_t M, int32_t K
  *   w [N][ldw] int8, w_scale [N] fp32 (the value of one code of that channel);
  *   bias [N] fp32 or NULL; y [M][ldy] in elem, columns N .. ldy-1 left as they were.
  * K, ldq and ldw are multiples of 16, K <= 131056 (so |sum| < 2^31).  M, N >= 0;
- * K == 0 gives the bias.
+ * K == 0 gives the bias.  Rows that begin with a cache line (ldq, ldw multiples
+ * of 128) are read fastest.
  */
 vla_status vla_int8_gemm(const int8_t* q, int64_t ldq, const float* r, const int8_t* w, int64_t ldw,
                          const float* w_scale, const float* bias, int32_t M, int32_t N, int32_t K, int32_t elem,
