@@ -370,17 +370,40 @@ def _gpu(x) -> Optional[int]:
     return x.data_ptr()
 
 
+def _direct(index: int, stream) -> bool:
+    """Whether a call may go to the current stream of the current device as it is."""
+    return stream is None and index == (_now or _bind_torch())[0]()
+
+
 def quantize_tokens(elem: int, x, M: int, K: int, ldx: int, q, ldq: int, r, stream=None):
     """Per-token int8 codes q [M][ldq] and absolute maxima r [M] of x [M][ldx]
     (elem: 0 fp32, 1 bf16)."""
-    _launch(lib().vla_quantize_tokens, _device(x), stream, elem, _gpu(x), M, K, ldx, _gpu(q), ldq, _gpu(r))
+    f = (_lib or lib()).vla_quantize_tokens
+    # Tensors on the current device: without the general path's half a microsecond.
+    try:
+        if x.is_cuda and q.is_cuda and r.is_cuda and _direct(i := x.get_device(), stream):
+            if st := f(elem, x.data_ptr(), M, K, ldx, q.data_ptr(), ldq, r.data_ptr(), _now[1](i)):
+                _check(st)
+            return
+    except AttributeError:   # an address
+        pass
+    _launch(f, _device(x), stream, elem, _gpu(x), M, K, ldx, _gpu(q), ldq, _gpu(r))
 
 
 def int8_gemm(q, ldq: int, r, w, ldw: int, w_scale, bias, M: int, N: int, K: int, elem: int, y, ldy: int, stream=None):
     """y [M][ldy] = (q w^T) * (w_scale[n] * r[m] / 127) + bias: int8 codes q, r of
     quantize_tokens, int8 weights w [N][ldw] with a scale per channel."""
-    _launch(lib().vla_int8_gemm, _device(q), stream, _gpu(q), ldq, _gpu(r), _gpu(w), ldw, _gpu(w_scale), _gpu(bias), M, N, K, elem,
-            _gpu(y), ldy)
+    f = (_lib or lib()).vla_int8_gemm
+    try:
+        if (q.is_cuda and r.is_cuda and w.is_cuda and w_scale.is_cuda and y.is_cuda and (bias is None or bias.is_cuda)
+                and _direct(i := q.get_device(), stream)):
+            if st := f(q.data_ptr(), ldq, r.data_ptr(), w.data_ptr(), ldw, w_scale.data_ptr(),
+                       None if bias is None else bias.data_ptr(), M, N, K, elem, y.data_ptr(), ldy, _now[1](i)):
+                _check(st)
+            return
+    except AttributeError:
+        pass
+    _launch(f, _device(q), stream, _gpu(q), ldq, _gpu(r), _gpu(w), ldw, _gpu(w_scale), _gpu(bias), M, N, K, elem, _gpu(y), ldy)
 
 
 class KVPages:
@@ -409,8 +432,15 @@ class KVBatch:
 
 def kv_pages_write(pages: KVPages, batch: KVBatch, elem: int, k, v, token_stride: int, head_stride: int, stream=None):
     """The new tokens' keys and values into their pages, quantised as the pages are."""
-    _launch(lib().vla_kv_pages_write, pages.device, stream, pages._ref, batch._ref, elem, _gpu(k), _gpu(v), token_stride,
-            head_stride)
+    f = (_lib or lib()).vla_kv_pages_write
+    try:
+        if k.is_cuda and v.is_cuda and _direct(pages.device, stream):
+            if st := f(pages._ref, batch._ref, elem, k.data_ptr(), v.data_ptr(), token_stride, head_stride, _now[1](pages.device)):
+                _check(st)
+            return
+    except AttributeError:
+        pass
+    _launch(f, pages.device, stream, pages._ref, batch._ref, elem, _gpu(k), _gpu(v), token_stride, head_stride)
 
 
 def kv_pages_read(pages: KVPages, batch: KVBatch, rows: int, elem: int, k_out, v_out, stream=None):
@@ -429,8 +459,19 @@ def paged_attention(pages: KVPages, batch: KVBatch, n_heads: int, elem: int, q, 
                     causal: bool = False, window: int = 0, lse=None, workspace=None, workspace_bytes: int = 0,
                     stream=None):
     """Attention of the new tokens q [n_tokens][ldq] over the pages of their requests."""
-    _launch(lib().vla_paged_attention, pages.device, stream, pages._ref, batch._ref, n_heads, elem, _gpu(q), ldq, _gpu(o),
-            ldo, float(scale), int(bool(causal)), int(window), _gpu(lse), _gpu(workspace), workspace_bytes)
+    f, scale, causal, window = (_lib or lib()).vla_paged_attention, float(scale), 1 if causal else 0, int(window)
+    try:
+        if (q.is_cuda and o.is_cuda and (lse is None or lse.is_cuda) and (workspace is None or workspace.is_cuda)
+                and _direct(pages.device, stream)):
+            if st := f(pages._ref, batch._ref, n_heads, elem, q.data_ptr(), ldq, o.data_ptr(), ldo, scale, causal, window,
+                       None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                       workspace_bytes, _now[1](pages.device)):
+                _check(st)
+            return
+    except AttributeError:
+        pass
+    _launch(f, pages.device, stream, pages._ref, batch._ref, n_heads, elem, _gpu(q), ldq, _gpu(o), ldo, scale, causal, window,
+            _gpu(lse), _gpu(workspace), workspace_bytes)
 
 
 # ---- test-only per-kernel entries (include/vla_test.h) ---------------------
